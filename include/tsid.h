@@ -506,6 +506,123 @@ typedef struct {
 tsid_status tsid_set_timing(tsid_ctx *ctx, int every);
 tsid_status tsid_get_timing(const tsid_ctx *ctx, tsid_timing *out);
 
+/* ------------------------------------------------------------------------
+ * Operators on factor rows: a table's rows by id, and the probabilities that
+ * factors give over all items (rows of H: users or any queries; rows of F: all
+ * items), with their gradients.  They need no template.
+ *
+ * Conventions of these calls:
+ *  - Factor tables are DEVICE, fp32 or bf16 (prec), k per row with k one of 8,
+ *    16, 32, 64, 128, and ld elements from one row to the next (ld >= k);
+ *    tables and rows are 16-byte aligned.  All tables of a call have one type.
+ *  - Every call is asynchronous on hip_stream (a hipStream_t of the context's
+ *    device; NULL is the device's default stream) and allocates nothing, so it
+ *    can be captured into a graph.  Scratch comes from the caller: `ws`, DEVICE,
+ *    256-byte aligned, of at least the size that the call's *_workspace function
+ *    gives; its contents need no care before or after, but two calls that may
+ *    run at once (other streams, graphs replayed at once) need one each.
+ *  - The context's other streams and state are not used, and the calling
+ *    thread's current device is left as it was.
+ *  - ids are int32.  -1 stands for no item.  Another id outside the table is
+ *    treated as -1 and reported as E_RANGE by the next tsid_rows_check.
+ *  - Sums are fp32 or fp64 in a fixed order, without atomics: results repeat
+ *    bit for bit.  Outputs must not overlap inputs or one another.
+ *  - Errors returned here: E_INVAL (NULL or misaligned pointer, bad size, k or
+ *    option, workspace too small), E_DEVICE.  Empty sizes are allowed.
+ */
+typedef struct {
+    void *p;       /* DEVICE */
+    int64_t rows;
+    int64_t ld;    /* elements from row to row */
+} tsid_rows;
+
+/* Wait for hip_stream, then return (and clear) what the row operators run so
+ * far on this context found on the device: E_RANGE, else TSID_OK.  Not while
+ * the stream is captured (E_STATE).  Errors: E_RANGE, E_DEVICE. */
+tsid_status tsid_rows_check(tsid_ctx *ctx, void *hip_stream);
+
+/* out[t] = scale * F[ids[t]] for t < out->rows (embedding lookup with
+ * scaling): the product in fp32, rounded once; zeros for id -1. */
+tsid_status tsid_lookup(tsid_ctx *ctx, int32_t prec, int32_t k, const tsid_rows *F, const int32_t *ids, float scale,
+                        const tsid_rows *out, void *hip_stream);
+
+/* Gradient of tsid_lookup in the table:
+ *   dF[i] = scale * sum_(t: ids[t] = i) G[t]    for every row i of dF
+ * (rows no id names get zeros).  The ids are sorted on the device (stable) and
+ * each row of dF is summed in fp32 in the order of t (rows named more than 64
+ * times: in pieces of the sorted list), rounded once and written once.
+ * G->rows < 2^31. */
+size_t tsid_lookup_grad_workspace(int64_t count, int64_t n, int32_t k);
+tsid_status tsid_lookup_grad(tsid_ctx *ctx, int32_t prec, int32_t k, const tsid_rows *G, const int32_t *ids,
+                             float scale, const tsid_rows *dF, void *ws, size_t ws_bytes, void *hip_stream);
+
+/* The scores of every item for every row,
+ *   z_ti = (scale h_t . f_i + bias_i) / temperature,
+ * and p_ti = exp z_ti / sum_i' exp z_ti'.
+ *  H     T rows.   F  n rows.  Both below 2^31 rows.
+ *  bias  DEVICE n floats or NULL (no bias); constant: it gets no gradient.  A
+ *        bias below -1e20 (-inf, the lowest float) excludes its item: p is 0
+ *        and its row of F is not used, whatever it holds.  Otherwise finite.
+ *  scale any finite number.  temperature: from 1e-6 to 1e6.
+ * Scores of a row all of whose items are excluded (or n = 0): log sum -inf,
+ * entropy 0, no best items, gradients 0.  A NaN in a row of H reaches that
+ * row's results.  Products of bf16 factors are exact and added in fp32; fp32
+ * factors are multiplied in three bf16 parts each, to about 2^-24 of the
+ * product of the rows' norms. */
+typedef struct {
+    tsid_rows H, F;
+    const float *bias;
+    int32_t k, prec;
+    float scale, temperature;
+} tsid_head;
+
+/* Log probabilities of given items, with entropy and the best items.  Every
+ * output may be NULL.
+ *  ids      DEVICE T x n_ids or NULL (n_ids = 0): logp[t, j] = log p_t,ids[t, j],
+ *           0 for id -1, -inf for an excluded item.
+ *  lse      T: log sum_i exp z_ti.     entropy  T: -sum_i p_ti log p_ti.
+ *  top      0 .. TSID_MAX_TOP: the items of the largest z, largest first, ties
+ *           to the lowest id; top_ids and top_logp are T x top (-1 and -inf
+ *           beyond the items that are not excluded).  Candidates are found with
+ *           scores in fp32 (blocks of 32 items by their largest score, 16 blocks
+ *           more than needed) and ranked by scores in fp64. */
+#define TSID_MAX_TOP 64
+size_t tsid_score_workspace(int64_t T, int64_t n, int32_t k, int32_t prec, int32_t top);
+tsid_status tsid_score(tsid_ctx *ctx, const tsid_head *head, const int32_t *ids, int32_t n_ids, int32_t top,
+                       float *lse, float *logp, float *entropy, int32_t *top_ids, float *top_logp, void *ws,
+                       size_t ws_bytes, void *hip_stream);
+
+/* Gradient of tsid_score's logp and entropy: with dz_ti = sum_j dlogp_tj
+ * ([i = ids_tj] - p_ti) - dentropy_t p_ti (log p_ti + entropy_t),
+ *   dH_t = scale / temperature * sum_i dz_ti f_i,
+ *   dF_i = scale / temperature * sum_t dz_ti h_t.
+ * An entry that is no item's, or an excluded item's, adds nothing; the same
+ * item listed twice adds twice.
+ *  lse, entropy  as tsid_score gave them (entropy and dentropy NULL together).
+ *  dlogp         T x n_ids (NULL with n_ids = 0).
+ *  dH, dF        tables of the factors' type, T and n rows; either may be NULL.
+ * n_ids * T < 2^31. */
+size_t tsid_head_grad_workspace(int64_t T, int64_t n, int32_t k, int32_t prec, int32_t n_ids);
+tsid_status tsid_score_grad(tsid_ctx *ctx, const tsid_head *head, const int32_t *ids, int32_t n_ids,
+                            const float *lse, const float *dlogp, const float *entropy, const float *dentropy,
+                            const tsid_rows *dH, const tsid_rows *dF, void *ws, size_t ws_bytes, void *hip_stream);
+
+/* Distillation from a teacher's best items: row t lists n_ids items and the
+ * teacher's logits of them.  With w_t the softmax of teacher_t / temperature
+ * over the listed items (without -1 and excluded ones),
+ *   loss_t = temperature^2 sum_j w_tj (log w_tj - log p_t,ids[t, j]),
+ * 0 for a row that lists none.  lse (not NULL) is kept for the gradient.
+ * Workspace: tsid_score_workspace with top 0. */
+tsid_status tsid_distill(tsid_ctx *ctx, const tsid_head *head, const int32_t *ids, int32_t n_ids,
+                         const float *teacher, float *loss, float *lse, void *ws, size_t ws_bytes, void *hip_stream);
+
+/* Gradient of sum_t dloss_t loss_t in H and F (dz_ti = dloss_t temperature^2
+ * (p_ti - sum_j w_tj [i = ids_tj]), then as tsid_score_grad); dloss: T.
+ * Workspace: tsid_head_grad_workspace. */
+tsid_status tsid_distill_grad(tsid_ctx *ctx, const tsid_head *head, const int32_t *ids, int32_t n_ids,
+                              const float *teacher, const float *lse, const float *dloss, const tsid_rows *dH,
+                              const tsid_rows *dF, void *ws, size_t ws_bytes, void *hip_stream);
+
 /* Index structures of the current template, copied to host_dst (HOST) for
  * bit-exact checks.  which / element type / count:
  *   TSID_IDX_ROW_MAP int32 m      TSID_IDX_COL_MAP int32 n

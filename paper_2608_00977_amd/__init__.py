@@ -5,6 +5,7 @@ extension of Stage II, as hand-written HIP behind the C ABI of
 from .binding import (  # noqa: F401
     Tsid,
     TsidError,
+    Scores,
     make_opts,
     make_adam_opts,
     tsid_chunk_plan,

@@ -13,7 +13,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
-from typing import Optional
+from typing import NamedTuple, Optional
 
 import numpy as np
 import torch  # imported before libtsid so both share one HIP runtime
@@ -63,6 +63,24 @@ class tsid_dense_info(C.Structure):
     _fields_ = [("cells", C.c_int64), ("tiles", C.c_int64), ("stripes", C.c_int64 * 2)]
 
 
+class tsid_rows(C.Structure):
+    _fields_ = [("p", C.c_void_p), ("rows", C.c_int64), ("ld", C.c_int64)]
+
+
+class tsid_head(C.Structure):
+    _fields_ = [("H", tsid_rows), ("F", tsid_rows), ("bias", C.c_void_p), ("k", C.c_int32),
+                ("prec", C.c_int32), ("scale", C.c_float), ("temperature", C.c_float)]
+
+
+class Scores(NamedTuple):
+    """Results of Tsid.score (None: not asked for)."""
+    lse: torch.Tensor
+    logp: Optional[torch.Tensor]
+    entropy: Optional[torch.Tensor]
+    top_ids: Optional[torch.Tensor]
+    top_logp: Optional[torch.Tensor]
+
+
 _lib: Optional[C.CDLL] = None
 
 
@@ -104,6 +122,16 @@ def lib() -> C.CDLL:
         "tsid_sync": (C.c_int, [P]),
         "tsid_export_index": (C.c_int, [P, C.c_int, P, sz]),
         "tsid_chunk_plan": (i32, [P, i64, i32, i64, P, i32]),
+        "tsid_rows_check": (C.c_int, [P, P]),
+        "tsid_lookup": (C.c_int, [P, i32, i32, P, P, C.c_float, P, P]),
+        "tsid_lookup_grad_workspace": (sz, [i64, i64, i32]),
+        "tsid_lookup_grad": (C.c_int, [P, i32, i32, P, P, C.c_float, P, P, sz, P]),
+        "tsid_score_workspace": (sz, [i64, i64, i32, i32, i32]),
+        "tsid_score": (C.c_int, [P, P, P, i32, i32, P, P, P, P, P, P, sz, P]),
+        "tsid_head_grad_workspace": (sz, [i64, i64, i32, i32, i32]),
+        "tsid_score_grad": (C.c_int, [P, P, P, i32, P, P, P, P, P, P, P, sz, P]),
+        "tsid_distill": (C.c_int, [P, P, P, i32, P, P, P, P, sz, P]),
+        "tsid_distill_grad": (C.c_int, [P, P, P, i32, P, P, P, P, P, P, sz, P]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(L, name)
@@ -254,6 +282,58 @@ def tsid_chunk_plan(counts: np.ndarray, n_chunks: int = 0, max_entries: int = 0)
     if nc < 0:
         raise TsidError(E_INVAL, "tsid_chunk_plan")
     return bounds[:nc + 1].copy()
+
+
+# Row operators: pointers are device addresses, ``rows`` arguments tsid_rows
+# structures, ``stream`` a hipStream_t handle (0: the device's default stream).
+def tsid_rows_check(ctx, stream: int = 0) -> int:
+    return lib().tsid_rows_check(ctx, stream)
+
+
+def tsid_lookup(ctx, prec, k, F: tsid_rows, ids, scale, out: tsid_rows, stream: int = 0) -> int:
+    return lib().tsid_lookup(ctx, prec, k, C.byref(F), ids, scale, C.byref(out), stream)
+
+
+def tsid_lookup_grad_workspace(count: int, n: int, k: int) -> int:
+    return lib().tsid_lookup_grad_workspace(count, n, k)
+
+
+def tsid_lookup_grad(ctx, prec, k, G: tsid_rows, ids, scale, dF: tsid_rows, ws, ws_bytes, stream: int = 0) -> int:
+    return lib().tsid_lookup_grad(ctx, prec, k, C.byref(G), ids, scale, C.byref(dF), ws, ws_bytes, stream)
+
+
+def tsid_score_workspace(T: int, n: int, k: int, prec: int, top: int = 0) -> int:
+    return lib().tsid_score_workspace(T, n, k, prec, top)
+
+
+def tsid_score(ctx, head: tsid_head, ids, n_ids, top, lse, logp, entropy, top_ids, top_logp, ws, ws_bytes,
+               stream: int = 0) -> int:
+    return lib().tsid_score(ctx, C.byref(head), ids, n_ids, top, lse, logp, entropy, top_ids, top_logp, ws,
+                            ws_bytes, stream)
+
+
+def tsid_head_grad_workspace(T: int, n: int, k: int, prec: int, n_ids: int) -> int:
+    return lib().tsid_head_grad_workspace(T, n, k, prec, n_ids)
+
+
+def _ref(rows: Optional[tsid_rows]):
+    return None if rows is None else C.byref(rows)
+
+
+def tsid_score_grad(ctx, head: tsid_head, ids, n_ids, lse, dlogp, entropy, dentropy, dH, dF, ws, ws_bytes,
+                    stream: int = 0) -> int:
+    return lib().tsid_score_grad(ctx, C.byref(head), ids, n_ids, lse, dlogp, entropy, dentropy, _ref(dH), _ref(dF),
+                                 ws, ws_bytes, stream)
+
+
+def tsid_distill(ctx, head: tsid_head, ids, n_ids, teacher, loss, lse, ws, ws_bytes, stream: int = 0) -> int:
+    return lib().tsid_distill(ctx, C.byref(head), ids, n_ids, teacher, loss, lse, ws, ws_bytes, stream)
+
+
+def tsid_distill_grad(ctx, head: tsid_head, ids, n_ids, teacher, lse, dloss, dH, dF, ws, ws_bytes,
+                      stream: int = 0) -> int:
+    return lib().tsid_distill_grad(ctx, C.byref(head), ids, n_ids, teacher, lse, dloss, _ref(dH), _ref(dF), ws,
+                                   ws_bytes, stream)
 
 
 # ------------------------------------------------------------ convenience
@@ -458,6 +538,175 @@ class Tsid:
                                           basis.shape[0], _ptr(F_free),
                                           _ptr(C_out) if C_out is not None else None, C.byref(opts))
         self._check(st, "tsid_extend_chunk_adam")
+
+    # ------------------------------------------------------ row operators
+    #
+    # They run on torch's current stream of the context's device, and their
+    # outputs and scratch come from torch's allocator (so they may be captured
+    # into a graph, and calls on several streams share nothing).  Factor tables
+    # are fp32 or bf16 tensors of k = 8, 16, 32, 64 or 128 columns, rows of any
+    # 16-byte aligned stride.
+
+    def _stream(self) -> int:
+        return torch.cuda.current_stream(self.device).cuda_stream
+
+    def _on_device(self, what: str, x: torch.Tensor, dtype=None):
+        if not isinstance(x, torch.Tensor) or x.device.type != "cuda" or x.device.index != self.device:
+            raise TsidError(E_INVAL, what, f"must be a tensor on cuda:{self.device}")
+        if dtype is not None and (x.dtype != dtype or not x.is_contiguous()):
+            raise TsidError(E_INVAL, what, f"must be contiguous {dtype}")
+
+    def _rows(self, what: str, x: torch.Tensor, like: Optional[torch.Tensor] = None) -> tsid_rows:
+        self._on_device(what, x)
+        if x.dim() != 2 or x.dtype not in (torch.float32, torch.bfloat16) or (x.shape[0] and x.stride(1) != 1):
+            raise TsidError(E_INVAL, what, "must be a 2-d fp32 or bf16 tensor with contiguous rows")
+        if like is not None and (x.dtype != like.dtype or x.shape[1] != like.shape[1]):
+            raise TsidError(E_INVAL, what, "differs in type or rank from the other factors")
+        return tsid_rows(x.data_ptr(), x.shape[0], x.stride(0) if x.shape[0] > 1 else x.shape[1])
+
+    def _scratch(self, nbytes: int) -> torch.Tensor:
+        # +255: the start is moved to a 256-byte boundary
+        return torch.empty(nbytes + 255, dtype=torch.uint8, device=f"cuda:{self.device}")
+
+    def _head(self, H, F, scale, bias, temperature=1.0) -> tsid_head:
+        h, f = self._rows("H", H), self._rows("F", F, H)
+        if bias is not None:
+            self._on_device("bias", bias, torch.float32)
+            if bias.shape != (F.shape[0],):
+                raise TsidError(E_INVAL, "bias", "must have one value per row of F")
+        return tsid_head(h, f, _ptr(bias), H.shape[1], BF16 if H.dtype == torch.bfloat16 else FP32, float(scale),
+                         float(temperature))
+
+    def _listed(self, H, ids, *arrays):
+        """Checks T x m arrays; returns m."""
+        if ids is None:
+            if any(a is not None for _, a in arrays):
+                raise TsidError(E_INVAL, "ids", "is None")
+            return 0
+        self._on_device("ids", ids, torch.int32)
+        if ids.dim() != 2 or ids.shape[0] != H.shape[0]:
+            raise TsidError(E_INVAL, "ids", "must be 2-d with one row per row of H")
+        for what, a in arrays:
+            self._on_device(what, a, torch.float32)
+            if a.shape != ids.shape:
+                raise TsidError(E_INVAL, what, "must have the shape of ids")
+        return ids.shape[1]
+
+    def _per_row(self, H, *arrays):
+        for what, a in arrays:
+            self._on_device(what, a, torch.float32)
+            if a.shape != (H.shape[0],):
+                raise TsidError(E_INVAL, what, "must have one value per row of H")
+
+    def _new(self, shape, dtype=torch.float32) -> torch.Tensor:
+        return torch.empty(shape, dtype=dtype, device=f"cuda:{self.device}")
+
+    def rows_check(self):
+        """Waits for the current stream and raises TSID_E_RANGE if a row
+        operator met an id outside its table (tsid_rows_check)."""
+        self._check(tsid_rows_check(self.ctx, self._stream()), "tsid_rows_check")
+
+    def lookup(self, F: torch.Tensor, ids: torch.Tensor, scale: float = 1.0,
+               out: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """Rows of F by id, scaled; zeros for id -1 (tsid_lookup)."""
+        f = self._rows("F", F)
+        self._on_device("ids", ids, torch.int32)
+        if out is None:
+            out = self._new((ids.numel(), F.shape[1]), F.dtype)
+        o = self._rows("out", out, F)
+        if o.rows != ids.numel():
+            raise TsidError(E_INVAL, "out", "must have one row per id")
+        self._check(tsid_lookup(self.ctx, BF16 if F.dtype == torch.bfloat16 else FP32, F.shape[1], f, _ptr(ids),
+                                float(scale), o, self._stream()), "tsid_lookup")
+        return out
+
+    def lookup_grad(self, G: torch.Tensor, ids: torch.Tensor, n: int, scale: float = 1.0,
+                    out: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """Gradient of lookup in its table of n rows: the rows of G summed by
+        id (tsid_lookup_grad)."""
+        g = self._rows("G", G)
+        self._on_device("ids", ids, torch.int32)
+        if g.rows != ids.numel():
+            raise TsidError(E_INVAL, "ids", "must have one id per row of G")
+        if out is None:
+            out = self._new((int(n), G.shape[1]), G.dtype)
+        o = self._rows("out", out, G)
+        if o.rows != n:
+            raise TsidError(E_INVAL, "out", "must have n rows")
+        nbytes = tsid_lookup_grad_workspace(g.rows, o.rows, G.shape[1])
+        ws = self._scratch(nbytes)
+        self._check(tsid_lookup_grad(self.ctx, BF16 if G.dtype == torch.bfloat16 else FP32, G.shape[1], g, _ptr(ids),
+                                     float(scale), o, (_ptr(ws) + 255) & ~255, nbytes, self._stream()),
+                    "tsid_lookup_grad")
+        return out
+
+    def score(self, H: torch.Tensor, F: torch.Tensor, ids: Optional[torch.Tensor] = None, scale: float = 1.0,
+              bias: Optional[torch.Tensor] = None, top: int = 0, entropy: bool = False) -> Scores:
+        """Log sums, log probabilities of the items `ids` (T x m), entropy and
+        the `top` best items of every row of H over all rows of F (tsid_score)."""
+        head = self._head(H, F, scale, bias)
+        m, T, top = self._listed(H, ids), H.shape[0], int(top)
+        r = Scores(self._new(T), self._new((T, m)) if ids is not None else None, self._new(T) if entropy else None,
+                   self._new((T, max(top, 0)), torch.int32) if top else None,
+                   self._new((T, max(top, 0))) if top else None)
+        nbytes = tsid_score_workspace(T, F.shape[0], head.k, head.prec, top)
+        ws = self._scratch(nbytes)
+        self._check(tsid_score(self.ctx, head, _ptr(ids), m, top, _ptr(r.lse), _ptr(r.logp), _ptr(r.entropy),
+                               _ptr(r.top_ids), _ptr(r.top_logp), (_ptr(ws) + 255) & ~255, nbytes, self._stream()),
+                    "tsid_score")
+        return r
+
+    def _grads(self, H, F, want_H, want_F):
+        dH = torch.empty_like(H, memory_format=torch.contiguous_format) if want_H else None
+        dF = torch.empty_like(F, memory_format=torch.contiguous_format) if want_F else None
+        return dH, dF, None if dH is None else self._rows("dH", dH), None if dF is None else self._rows("dF", dF)
+
+    def score_grad(self, H: torch.Tensor, F: torch.Tensor, lse: torch.Tensor, ids: Optional[torch.Tensor] = None,
+                   dlogp: Optional[torch.Tensor] = None, entropy: Optional[torch.Tensor] = None,
+                   dentropy: Optional[torch.Tensor] = None, scale: float = 1.0,
+                   bias: Optional[torch.Tensor] = None, want_H: bool = True, want_F: bool = True):
+        """(dH, dF): the gradients in H and F of score's log probabilities
+        (weights dlogp) and entropy (weights dentropy); lse and entropy as
+        score gave them (tsid_score_grad)."""
+        head = self._head(H, F, scale, bias)
+        m = self._listed(H, ids, *([("dlogp", dlogp)] if ids is not None or dlogp is not None else []))
+        self._per_row(H, ("lse", lse), *([] if entropy is None else [("entropy", entropy)]),
+                      *([] if dentropy is None else [("dentropy", dentropy)]))
+        dH, dF, rh, rf = self._grads(H, F, want_H, want_F)
+        nbytes = tsid_head_grad_workspace(H.shape[0], F.shape[0], head.k, head.prec, m)
+        ws = self._scratch(nbytes)
+        self._check(tsid_score_grad(self.ctx, head, _ptr(ids), m, _ptr(lse), _ptr(dlogp), _ptr(entropy),
+                                    _ptr(dentropy), rh, rf, (_ptr(ws) + 255) & ~255, nbytes, self._stream()),
+                    "tsid_score_grad")
+        return dH, dF
+
+    def distill(self, H: torch.Tensor, F: torch.Tensor, ids: torch.Tensor, teacher: torch.Tensor,
+                scale: float = 1.0, temperature: float = 1.0, bias: Optional[torch.Tensor] = None):
+        """(loss, lse) per row of H: the divergence from a teacher's logits of
+        the items `ids` (both T x m) to the factors' probabilities (tsid_distill)."""
+        head = self._head(H, F, scale, bias, temperature)
+        m = self._listed(H, ids, ("teacher", teacher))
+        loss, lse = self._new(H.shape[0]), self._new(H.shape[0])
+        nbytes = tsid_score_workspace(H.shape[0], F.shape[0], head.k, head.prec, 0)
+        ws = self._scratch(nbytes)
+        self._check(tsid_distill(self.ctx, head, _ptr(ids), m, _ptr(teacher), _ptr(loss), _ptr(lse),
+                                 (_ptr(ws) + 255) & ~255, nbytes, self._stream()), "tsid_distill")
+        return loss, lse
+
+    def distill_grad(self, H: torch.Tensor, F: torch.Tensor, ids: torch.Tensor, teacher: torch.Tensor,
+                     lse: torch.Tensor, dloss: torch.Tensor, scale: float = 1.0, temperature: float = 1.0,
+                     bias: Optional[torch.Tensor] = None, want_H: bool = True, want_F: bool = True):
+        """(dH, dF): the gradients in H and F of sum(dloss * loss); lse as
+        distill gave it (tsid_distill_grad)."""
+        head = self._head(H, F, scale, bias, temperature)
+        m = self._listed(H, ids, ("teacher", teacher))
+        self._per_row(H, ("lse", lse), ("dloss", dloss))
+        dH, dF, rh, rf = self._grads(H, F, want_H, want_F)
+        nbytes = tsid_head_grad_workspace(H.shape[0], F.shape[0], head.k, head.prec, m)
+        ws = self._scratch(nbytes)
+        self._check(tsid_distill_grad(self.ctx, head, _ptr(ids), m, _ptr(teacher), _ptr(lse), _ptr(dloss), rh, rf,
+                                      (_ptr(ws) + 255) & ~255, nbytes, self._stream()), "tsid_distill_grad")
+        return dH, dF
 
     def sync(self):
         st = tsid_sync(self.ctx)

@@ -11,6 +11,7 @@
 #include <vector>
 
 #include "internal.h"
+#include "rows.h"
 
 namespace tsid {
 
@@ -286,6 +287,7 @@ struct tsid_ctx {
     int32_t row_blocks = 0;           // tsid_set_row_blocks: 0 automatic, 1 off, n forced
     int32_t used_blocks = 1;          // row blocks of the last fit's Q pass
     void *noalloc_scratch = nullptr;  // device address of this device's scratch array
+    int32_t *rows_err = nullptr;      // error slots of the row operators
 };
 
 namespace {
@@ -2718,6 +2720,124 @@ void export_index(const tsid_ctx *c, int which, void *dst, size_t bytes) {
     }
 }
 
+// ---------------------------------------------------------- row operators
+
+// The calling thread's current device, put back at the end.
+struct DeviceGuard {
+    int before = -1;
+    explicit DeviceGuard(int device) {
+        TSID_HIP(hipGetDevice(&before));
+        if (before != device) TSID_HIP(hipSetDevice(device));
+        else before = -1;
+    }
+    ~DeviceGuard() {
+        if (before >= 0) (void)hipSetDevice(before);
+    }
+    DeviceGuard(const DeviceGuard &) = delete;
+    DeviceGuard &operator=(const DeviceGuard &) = delete;
+};
+
+// guarded() for calls that leave the current device as it was.
+template <typename F>
+tsid_status guarded_here(tsid_ctx *c, F &&f) {
+    if (!c) return TSID_E_INVAL;
+    try {
+        DeviceGuard here(c->device);
+        f();
+        c->err.clear();
+        return TSID_OK;
+    } catch (const Error &e) {
+        c->err = e.msg;
+        return e.st;
+    } catch (const std::exception &e) {
+        c->err = e.what();
+        return TSID_E_DEVICE;
+    }
+}
+
+constexpr int64_t kMaxRows = (int64_t(1) << 31) - 1;
+
+void check_rank_prec(int32_t k, int32_t prec) {
+    if (!valid_rank(k)) fail(TSID_E_INVAL, "k must be 8, 16, 32, 64 or 128");
+    if (prec != TSID_FP32 && prec != TSID_BF16) fail(TSID_E_INVAL, "bad precision");
+}
+
+Rows check_rows(const tsid_rows *r, int32_t k, int32_t prec, const char *what) {
+    const std::string name(what);
+    if (!r) fail(TSID_E_INVAL, name + " is NULL");
+    if (r->rows < 0 || r->rows > kMaxRows) fail(TSID_E_INVAL, name + ": bad row count");
+    if (r->rows == 0) return Rows{r->p, 0, k};
+    if (!r->p) fail(TSID_E_INVAL, name + ": NULL pointer");
+    check_aligned(r->p, what);
+    if (r->ld < k || r->ld > kMaxRows) fail(TSID_E_INVAL, name + ": ld must be at least k");
+    if (r->ld % (prec == TSID_BF16 ? 8 : 4) != 0) fail(TSID_E_INVAL, name + ": rows must be 16-byte aligned");
+    return Rows{r->p, r->rows, r->ld};
+}
+
+void check_array(const void *p, int64_t count, const char *what) {
+    if (count > 0 && !p) fail(TSID_E_INVAL, std::string(what) + " is NULL");
+    if (reinterpret_cast<uintptr_t>(p) % 4 != 0) fail(TSID_E_INVAL, std::string(what) + " must be 4-byte aligned");
+}
+
+void check_workspace(const void *ws, size_t bytes, size_t needed) {
+    if (!ws || reinterpret_cast<uintptr_t>(ws) % 256 != 0)
+        fail(TSID_E_INVAL, "the workspace must be 256-byte aligned device memory");
+    if (bytes < needed)
+        fail(TSID_E_INVAL, "the workspace has " + std::to_string(bytes) + " bytes of " + std::to_string(needed));
+}
+
+Head check_head(const tsid_head *h) {
+    if (!h) fail(TSID_E_INVAL, "head is NULL");
+    check_rank_prec(h->k, h->prec);
+    if (!std::isfinite(h->scale)) fail(TSID_E_INVAL, "scale must be finite");
+    if (!(h->temperature >= 1e-6f && h->temperature <= 1e6f)) fail(TSID_E_INVAL, "temperature must be in [1e-6, 1e6]");
+    Head o{};
+    o.H = check_rows(&h->H, h->k, h->prec, "H");
+    o.F = check_rows(&h->F, h->k, h->prec, "F");
+    check_array(h->bias, 0, "bias");
+    o.bias = h->bias;
+    o.k = h->k;
+    o.prec = h->prec;
+    o.scale = h->scale / h->temperature;
+    if (!std::isfinite(o.scale)) fail(TSID_E_INVAL, "scale / temperature must be finite");
+    o.bias_scale = 1.f / h->temperature;
+    return o;
+}
+
+void check_listed(const Head &h, const int32_t *ids, int32_t n_ids) {
+    if (n_ids < 0 || h.H.count * n_ids > kMaxRows) fail(TSID_E_INVAL, "n_ids must be >= 0, with n_ids rows below 2^31");
+    check_array(ids, h.H.count * n_ids, "ids");
+}
+
+// Common part of the gradients: the outputs' tables and the workspace.
+void check_grads(const Head &h, const tsid_head *head, int32_t n_ids, const tsid_rows *dH, const tsid_rows *dF,
+                 const void *ws, size_t bytes, HeadGrad &g) {
+    if (dH) {
+        g.dH = check_rows(dH, head->k, head->prec, "dH");
+        if (g.dH.count != h.H.count) fail(TSID_E_INVAL, "dH must have the rows of H");
+    }
+    if (dF) {
+        g.dF = check_rows(dF, head->k, head->prec, "dF");
+        if (g.dF.count != h.F.count) fail(TSID_E_INVAL, "dF must have the rows of F");
+    }
+    check_workspace(ws, bytes, head_grad_workspace(h.H.count, h.F.count, h.k, h.prec, n_ids));
+}
+
+bool sizes_ok(int64_t T, int64_t n, int32_t k) { return T >= 0 && T <= kMaxRows && n >= 0 && n <= kMaxRows && valid_rank(k); }
+
+void rows_check(tsid_ctx *c, hipStream_t s) {
+    hipStreamCaptureStatus cap = hipStreamCaptureStatusNone;
+    TSID_HIP(hipStreamIsCapturing(s, &cap));
+    if (cap != hipStreamCaptureStatusNone) fail(TSID_E_STATE, "the stream is being captured");
+    int32_t e[ERR_SLOTS];
+    TSID_HIP(hipMemcpyAsync(e, c->rows_err, sizeof(e), hipMemcpyDeviceToHost, s));
+    TSID_HIP(hipStreamSynchronize(s));
+    if (!e[ERR_RANGE]) return;
+    fill_i32(c->rows_err, ERR_SLOTS, 0, s);
+    TSID_HIP(hipStreamSynchronize(s));
+    fail(TSID_E_RANGE, "row operators: id out of range");
+}
+
 }  // namespace
 
 // ================================================================ C ABI
@@ -2747,6 +2867,8 @@ tsid_status tsid_create(int device, void *hip_stream, size_t max_device_bytes, t
         c->err_dev = c->arena.alloc<int32_t>(ERR_SLOTS);
         TSID_HIP(hipHostMalloc((void **)&c->err_host, ERR_SLOTS * sizeof(int32_t), hipHostMallocDefault));
         TSID_HIP(hipMemset(c->err_dev, 0, ERR_SLOTS * sizeof(int32_t)));
+        c->rows_err = c->arena.alloc<int32_t>(ERR_SLOTS);
+        TSID_HIP(hipMemset(c->rows_err, 0, ERR_SLOTS * sizeof(int32_t)));
         c->noalloc_scratch = noalloc_scratch_on(device);
     });
     if (st != TSID_OK) {
@@ -2778,6 +2900,7 @@ void tsid_destroy(tsid_ctx *c) {
     }
     for (hipEvent_t e : c->events) (void)hipEventDestroy(e);
     c->arena.release(c->err_dev);
+    c->arena.release(c->rows_err);
     if (c->err_host) (void)hipHostFree(c->err_host);
     if (c->small_host) (void)hipHostFree(c->small_host);
     if (c->h2d) (void)hipStreamDestroy(c->h2d);
@@ -2923,6 +3046,156 @@ tsid_status tsid_sync(tsid_ctx *c) {
 tsid_status tsid_export_index(const tsid_ctx *c, int which, void *host_dst, size_t bytes) {
     tsid_ctx *mc = const_cast<tsid_ctx *>(c);
     return guarded(mc, [&]() { export_index(c, which, host_dst, bytes); });
+}
+
+tsid_status tsid_rows_check(tsid_ctx *c, void *hip_stream) {
+    return guarded_here(c, [&]() { rows_check(c, static_cast<hipStream_t>(hip_stream)); });
+}
+
+tsid_status tsid_lookup(tsid_ctx *c, int32_t prec, int32_t k, const tsid_rows *F, const int32_t *ids, float scale,
+                        const tsid_rows *out, void *hip_stream) {
+    return guarded_here(c, [&]() {
+        check_rank_prec(k, prec);
+        const Rows f = check_rows(F, k, prec, "F"), o = check_rows(out, k, prec, "out");
+        check_array(ids, o.count, "ids");
+        launch_lookup(k, prec, f, ids, scale, o, c->rows_err, static_cast<hipStream_t>(hip_stream));
+    });
+}
+
+size_t tsid_lookup_grad_workspace(int64_t count, int64_t n, int32_t k) {
+    if (!sizes_ok(count, n, k)) return 0;
+    SumPlan p{};
+    p.entries = count;
+    p.n = n;
+    p.k = k;
+    Carve carve;
+    carve_sum(p, carve);
+    return carve.used;
+}
+
+tsid_status tsid_lookup_grad(tsid_ctx *c, int32_t prec, int32_t k, const tsid_rows *G, const int32_t *ids,
+                             float scale, const tsid_rows *dF, void *ws, size_t ws_bytes, void *hip_stream) {
+    return guarded_here(c, [&]() {
+        check_rank_prec(k, prec);
+        const Rows g = check_rows(G, k, prec, "G"), o = check_rows(dF, k, prec, "dF");
+        check_array(ids, g.count, "ids");
+        check_workspace(ws, ws_bytes, tsid_lookup_grad_workspace(g.count, o.count, k));
+        SumPlan p{};
+        p.entries = g.count;
+        p.n = o.count;
+        p.k = k;
+        Carve carve{static_cast<char *>(ws)};
+        carve_sum(p, carve);
+        hipStream_t s = static_cast<hipStream_t>(hip_stream);
+        launch_sum_sort(p, ids, nullptr, c->rows_err, s);
+        SumArgs a{};
+        a.X = g;
+        a.per_row = 1;
+        a.scale = scale;
+        a.out = o;
+        launch_sum_rows(p, prec, a, s);
+    });
+}
+
+size_t tsid_score_workspace(int64_t T, int64_t n, int32_t k, int32_t prec, int32_t top) {
+    if (!sizes_ok(T, n, k) || (prec != TSID_FP32 && prec != TSID_BF16) || top < 0 || top > TSID_MAX_TOP) return 0;
+    return score_workspace(T, n, k, prec, top);
+}
+
+tsid_status tsid_score(tsid_ctx *c, const tsid_head *head, const int32_t *ids, int32_t n_ids, int32_t top,
+                       float *lse, float *logp, float *entropy, int32_t *top_ids, float *top_logp, void *ws,
+                       size_t ws_bytes, void *hip_stream) {
+    return guarded_here(c, [&]() {
+        const Head h = check_head(head);
+        check_listed(h, ids, n_ids);
+        if (top < 0 || top > TSID_MAX_TOP) fail(TSID_E_INVAL, "top must be in 0 .. 64");
+        if (top > 0 && h.H.count > 0 && (!top_ids || !top_logp)) fail(TSID_E_INVAL, "top_ids or top_logp is NULL");
+        for (const void *p : {(const void *)lse, (const void *)logp, (const void *)entropy, (const void *)top_ids,
+                              (const void *)top_logp})
+            check_array(p, 0, "an output");
+        check_workspace(ws, ws_bytes, score_workspace(h.H.count, h.F.count, h.k, h.prec, top));
+        ScoreOut o{};
+        o.ids = ids;
+        o.per_row = n_ids;
+        o.top = top;
+        o.lse = lse;
+        o.logp = n_ids > 0 ? logp : nullptr;
+        o.entropy = entropy;
+        o.top_ids = top_ids;
+        o.top_logp = top_logp;
+        run_score(h, o, ws, c->rows_err, static_cast<hipStream_t>(hip_stream));
+    });
+}
+
+size_t tsid_head_grad_workspace(int64_t T, int64_t n, int32_t k, int32_t prec, int32_t n_ids) {
+    if (!sizes_ok(T, n, k) || (prec != TSID_FP32 && prec != TSID_BF16) || n_ids < 0 || T * n_ids > kMaxRows) return 0;
+    return head_grad_workspace(T, n, k, prec, n_ids);
+}
+
+tsid_status tsid_score_grad(tsid_ctx *c, const tsid_head *head, const int32_t *ids, int32_t n_ids,
+                            const float *lse, const float *dlogp, const float *entropy, const float *dentropy,
+                            const tsid_rows *dH, const tsid_rows *dF, void *ws, size_t ws_bytes, void *hip_stream) {
+    return guarded_here(c, [&]() {
+        const Head h = check_head(head);
+        check_listed(h, ids, n_ids);
+        check_array(lse, h.H.count, "lse");
+        check_array(dlogp, h.H.count * n_ids, "dlogp");
+        if ((entropy == nullptr) != (dentropy == nullptr)) fail(TSID_E_INVAL, "entropy and dentropy go together");
+        check_array(entropy, 0, "entropy");
+        check_array(dentropy, 0, "dentropy");
+        HeadGrad g{};
+        g.ids = ids;
+        g.per_row = n_ids;
+        g.lse = lse;
+        g.dlogp = dlogp;
+        g.entropy = entropy;
+        g.dentropy = dentropy;
+        check_grads(h, head, n_ids, dH, dF, ws, ws_bytes, g);
+        run_head_grad(h, g, ws, c->rows_err, static_cast<hipStream_t>(hip_stream));
+    });
+}
+
+tsid_status tsid_distill(tsid_ctx *c, const tsid_head *head, const int32_t *ids, int32_t n_ids,
+                         const float *teacher, float *loss, float *lse, void *ws, size_t ws_bytes, void *hip_stream) {
+    return guarded_here(c, [&]() {
+        const Head h = check_head(head);
+        if (n_ids < 1) fail(TSID_E_INVAL, "n_ids must be >= 1");
+        check_listed(h, ids, n_ids);
+        check_array(teacher, h.H.count * n_ids, "teacher");
+        check_array(loss, h.H.count, "loss");
+        check_array(lse, h.H.count, "lse");
+        check_workspace(ws, ws_bytes, score_workspace(h.H.count, h.F.count, h.k, h.prec, 0));
+        DistillOut o{};
+        o.ids = ids;
+        o.per_row = n_ids;
+        o.teacher = teacher;
+        o.temperature = head->temperature;
+        o.loss = loss;
+        o.lse = lse;
+        run_distill(h, o, ws, c->rows_err, static_cast<hipStream_t>(hip_stream));
+    });
+}
+
+tsid_status tsid_distill_grad(tsid_ctx *c, const tsid_head *head, const int32_t *ids, int32_t n_ids,
+                              const float *teacher, const float *lse, const float *dloss, const tsid_rows *dH,
+                              const tsid_rows *dF, void *ws, size_t ws_bytes, void *hip_stream) {
+    return guarded_here(c, [&]() {
+        const Head h = check_head(head);
+        if (n_ids < 1) fail(TSID_E_INVAL, "n_ids must be >= 1");
+        check_listed(h, ids, n_ids);
+        check_array(teacher, h.H.count * n_ids, "teacher");
+        check_array(lse, h.H.count, "lse");
+        check_array(dloss, h.H.count, "dloss");
+        HeadGrad g{};
+        g.ids = ids;
+        g.per_row = n_ids;
+        g.lse = lse;
+        g.teacher = teacher;
+        g.dloss = dloss;
+        g.temperature = head->temperature;
+        check_grads(h, head, n_ids, dH, dF, ws, ws_bytes, g);
+        run_head_grad(h, g, ws, c->rows_err, static_cast<hipStream_t>(hip_stream));
+    });
 }
 
 int32_t tsid_chunk_plan(const int64_t *counts, int64_t n_free, int32_t n_chunks, int64_t max_entries,

@@ -1,0 +1,1269 @@
+// Probabilities over all items: z = scale H F^T + bias, p = softmax of each row.
+// Scores (log sum, log probabilities of given items, entropy, best items),
+// distillation, and the gradients of both in H and F.
+//
+// No score ever reaches memory.  Both directions stream tiles of 32 rows of one
+// side (Y) past rows of the other side that stay in registers (X), one wave per
+// 32 or 64 of them, and take S = Y X^T with v_mfma_f32_32x32x16_bf16, which leaves
+// lane l with column l % 32 (its own row of X) and 16 of the 32 rows of Y (rows
+// 8 (r / 4) + 4 (l / 32) + r % 4, r = 0 .. 15): a row's running maximum and sums
+// are the lane's own, without any exchange.
+//
+// fp32 factors are split into three bf16 parts each (8 + 8 + 8 bits, exact) and
+// multiplied part by part, six products for the nine (the other three are below
+// 2^-24 of the whole): 96 cycles of a SIMD per 64 scores at k = 128, where
+// v_mfma_f32_32x32x2_f32 takes 256.  bf16 factors take 16.
+//
+// Exponentials are base 2: p = 2^(c s - m) with c = |scale| log2 e (a negative
+// scale turns the sign of X).
+#include <algorithm>
+#include <cmath>
+#include <type_traits>
+
+#include "rows.h"
+
+namespace tsid {
+
+namespace {
+
+constexpr int kThreads = 256;
+constexpr double kLog2e = 1.4426950408889634074, kLn2 = 0.69314718055994530942;
+constexpr float kOff = -2e30f;    // the exponent's offset at an excluded item
+constexpr float kLeast = -1e30f;  // a running maximum before the first item
+
+typedef float f4 __attribute__((ext_vector_type(4)));
+typedef float f8 __attribute__((ext_vector_type(8)));
+typedef float f16 __attribute__((ext_vector_type(16)));
+typedef __bf16 b8 __attribute__((ext_vector_type(8)));
+typedef short s4 __attribute__((ext_vector_type(4)));
+
+// Sizes for rank K and NP bf16 parts per factor: k-steps of the scores, the
+// width of a row in LDS (at least one block of 32 coordinates, zeros beyond K)
+// and its stride (16 bytes of padding: 16 lanes' 16-byte reads of 16 rows, and
+// the transposing reads, fall on distinct banks).
+template <int K, int NP>
+struct Shape {
+    static constexpr int KS = K < 16 ? 1 : K / 16;
+    static constexpr int KW = K < 32 ? 32 : K;
+    static constexpr int NB = KW / 32;  // coordinate blocks of the gradients
+    static constexpr int RS = KW + 8;
+    static constexpr int CH = K / 8;    // 16-byte chunks of a row
+};
+
+// Eight factors as read: bf16 (NP = 1) or fp32 (NP = 3).
+template <int NP>
+struct Raw {
+    uint4 w[NP == 1 ? 1 : 2];
+};
+template <int NP>
+__device__ __forceinline__ Raw<NP> load_raw(const void *base, int64_t at) {
+    Raw<NP> r;
+    if constexpr (NP == 1) {
+        r.w[0] = *reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(base) + at);
+    } else {
+        const uint4 *p = reinterpret_cast<const uint4 *>(static_cast<const float *>(base) + at);
+        r.w[0] = p[0];
+        r.w[1] = p[1];
+    }
+    return r;
+}
+template <int NP>
+__device__ __forceinline__ Raw<NP> zero_raw() {
+    Raw<NP> r;
+    for (auto &w : r.w) w = make_uint4(0u, 0u, 0u, 0u);
+    return r;
+}
+
+// x = part[0] + part[1] + part[2], each rounded to nearest even from what the
+// ones before it leave (the differences are exact).
+__device__ __forceinline__ void split3(f8 x, b8 (&part)[3]) {
+    part[0] = __builtin_convertvector(x, b8);
+    x -= __builtin_convertvector(part[0], f8);
+    part[1] = __builtin_convertvector(x, b8);
+    x -= __builtin_convertvector(part[1], f8);
+    part[2] = __builtin_convertvector(x, b8);
+}
+template <int NP>
+__device__ __forceinline__ void parts_of(const Raw<NP> &r, b8 (&part)[NP]) {
+    if constexpr (NP == 1) {
+        part[0] = __builtin_bit_cast(b8, r.w[0]);
+    } else {
+        const f4 a = __builtin_bit_cast(f4, r.w[0]), b = __builtin_bit_cast(f4, r.w[1]);
+        split3(f8{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]}, part);
+    }
+}
+
+// acc += a b over the parts.
+template <int NP>
+__device__ __forceinline__ f16 product(const b8 (&a)[NP], const b8 (&b)[NP], f16 acc) {
+    if constexpr (NP == 3) {
+        acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[0], b[2], acc, 0, 0, 0);
+        acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[2], b[0], acc, 0, 0, 0);
+        acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[1], b[1], acc, 0, 0, 0);
+        acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[0], b[1], acc, 0, 0, 0);
+        acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[1], b[0], acc, 0, 0, 0);
+    }
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[0], b[0], acc, 0, 0, 0);
+}
+
+// One side of the scores.
+struct Side {
+    const void *p;
+    int64_t count, ld;
+    const float *bias;  // of the items, or null
+};
+
+// A tile of YT rows of Y in LDS: NP planes of bf16 parts, then an offset per row.
+template <int K, int NP, int YT>
+struct Tile {
+    using S = Shape<K, NP>;
+    static constexpr int kPlane = YT * S::RS;
+    static constexpr int kPer = (YT * S::CH + kThreads - 1) / kThreads;  // chunks per thread
+    static constexpr size_t kBytes = (size_t)NP * kPlane * 2 + YT * 16;
+    Raw<NP> raw[kPer];
+    float bias[kPer];
+
+    // Rows y0 .. y0 + YT - 1 into registers; zeros beyond the side and for excluded items.
+    __device__ __forceinline__ void load(const Side &Y, int64_t y0) {
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+            const int q = threadIdx.x + i * kThreads;
+            const int64_t row = y0 + q / S::CH;
+            raw[i] = zero_raw<NP>();
+            bias[i] = 0.f;
+            if ((YT * S::CH) % kThreads != 0 && q >= YT * S::CH) continue;
+            if (row < Y.count) {
+                raw[i] = load_raw<NP>(Y.p, row * Y.ld + (q % S::CH) * 8);
+                if (Y.bias) bias[i] = Y.bias[row];
+            }
+        }
+    }
+    __device__ __forceinline__ void store(const Side &Y, uint16_t *lds) const {
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+            const int q = threadIdx.x + i * kThreads;
+            if ((YT * S::CH) % kThreads != 0 && q >= YT * S::CH) continue;
+            b8 part[NP];
+            parts_of<NP>(bias[i] < kExcluded ? zero_raw<NP>() : raw[i], part);
+#pragma unroll
+            for (int p = 0; p < NP; ++p)
+                *reinterpret_cast<uint4 *>(lds + p * kPlane + (q / S::CH) * S::RS + (q % S::CH) * 8) =
+                    __builtin_bit_cast(uint4, part[p]);
+        }
+    }
+};
+
+// The rows x0 + l % 32 of X as B operands, turned if `turn`.
+template <int K, int NP>
+__device__ __forceinline__ void load_x(const Side &X, int64_t x0, bool turn, b8 (&x)[Shape<K, NP>::KS][NP]) {
+    const int lane = threadIdx.x & 63;
+    const int64_t row = x0 + (lane & 31);
+#pragma unroll
+    for (int s = 0; s < Shape<K, NP>::KS; ++s) {
+        const int c = 16 * s + 8 * (lane >> 5);
+        Raw<NP> r = zero_raw<NP>();
+        if (row < X.count && c < K && !(X.bias && X.bias[row] < kExcluded)) r = load_raw<NP>(X.p, row * X.ld + c);
+        if (turn) {
+            const uint32_t f = NP == 1 ? 0x80008000u : 0x80000000u;
+            for (auto &w : r.w) w = make_uint4(w.x ^ f, w.y ^ f, w.z ^ f, w.w ^ f);
+        }
+        parts_of<NP>(r, x[s]);
+    }
+}
+
+// S = Y X^T for the 32 rows of Y at `y` in LDS.
+template <int K, int NP, int YT>
+__device__ __forceinline__ f16 scores(const uint16_t *y, const b8 (&x)[Shape<K, NP>::KS][NP]) {
+    using S = Shape<K, NP>;
+    const int lane = threadIdx.x & 63;
+    const uint16_t *row = y + (lane & 31) * S::RS + 8 * (lane >> 5);
+    f16 acc = {};
+#pragma unroll
+    for (int s = 0; s < S::KS; ++s) {
+        b8 a[NP];
+#pragma unroll
+        for (int p = 0; p < NP; ++p)
+            a[p] = __builtin_bit_cast(b8, *reinterpret_cast<const uint4 *>(row + p * Tile<K, NP, YT>::kPlane + 16 * s));
+        acc = product<NP>(a, x[s], acc);
+    }
+    return acc;
+}
+
+// The row of a 32-row tile that a lane's r-th score belongs to (without 4 (l / 32)).
+__device__ __forceinline__ constexpr int tile_row(int r) { return 8 * (r / 4) + r % 4; }
+
+// ------------------------------------------------------------------ scores
+
+// Running maximum m (base-2 exponent), s = sum 2^(x - m), e = sum 2^(x - m) (x - m).
+struct Stat {
+    float m = kLeast, s = 0.f, e = 0.f;
+};
+
+__device__ __forceinline__ void merge(Stat &a, const Stat &b) {
+    const float m = fmaxf(a.m, b.m), da = a.m - m, db = b.m - m;
+    const float fa = __builtin_amdgcn_exp2f(da), fb = __builtin_amdgcn_exp2f(db);
+    a.e = (a.s > 0.f ? fmaf(a.s, da, a.e) * fa : 0.f) + (b.s > 0.f ? fmaf(b.s, db, b.e) * fb : 0.f);
+    a.s = a.s * fa + b.s * fb;
+    a.m = m;
+}
+
+// Takes 16 scores; returns the largest exponent.  MASKED: off[r] is added
+// (the items' bias, kOff where excluded), else nothing.
+template <bool ENT, bool MASKED>
+__device__ __forceinline__ float take(Stat &st, const f16 &acc, float c, const float *off) {
+    float x[16];
+    float top;
+    if constexpr (MASKED) {
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const f4 o = *reinterpret_cast<const f4 *>(off + 8 * q);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) x[4 * q + j] = fmaf(acc[4 * q + j], c, o[j]);
+        }
+        top = x[0];
+#pragma unroll
+        for (int r = 1; r < 16; ++r) top = fmaxf(top, x[r]);
+    } else {
+        top = acc[0];
+#pragma unroll
+        for (int r = 1; r < 16; ++r) top = fmaxf(top, acc[r]);
+        top *= c;
+    }
+    if (__any(top > st.m)) {
+        const float m = fmaxf(st.m, top), d = st.m - m, f = __builtin_amdgcn_exp2f(d);
+        if (ENT) st.e = fmaf(st.s, d, st.e) * f;
+        st.s *= f;
+        st.m = m;
+    }
+    float s0 = 0.f, s1 = 0.f, e0 = 0.f, e1 = 0.f;
+#pragma unroll
+    for (int r = 0; r < 16; r += 2) {
+        const float y0 = MASKED ? x[r] - st.m : fmaf(acc[r], c, -st.m);
+        const float y1 = MASKED ? x[r + 1] - st.m : fmaf(acc[r + 1], c, -st.m);
+        const float p0 = __builtin_amdgcn_exp2f(y0), p1 = __builtin_amdgcn_exp2f(y1);
+        s0 += p0;
+        s1 += p1;
+        if (ENT) {
+            e0 = fmaf(p0, y0, e0);
+            e1 = fmaf(p1, y1, e1);
+        }
+    }
+    st.s += s0 + s1;
+    if (ENT) st.e += e0 + e1;
+    return top;
+}
+
+struct ScoreK {
+    Side H, F;
+    float c;           // |scale| log2 e
+    int turn;
+    float bias_c;      // log2 e / temperature
+    int64_t t0;        // first row of this run
+    int64_t T;         // rows of this run
+    int64_t slice_items;
+    int32_t n_slices, n_tiles;
+    float4 *part;      // [slice][T]: m, s, e
+    float *blkmax;     // [item / 32][T], or null
+};
+
+// The slice and row tile of a workgroup: workgroups go to the 8 XCDs in turn,
+// so that the row tiles which read a slice of F run on one XCD and share its L2.
+__device__ __forceinline__ bool place(int32_t n_slices, int32_t n_tiles, int32_t &slice, int32_t &tile) {
+    const int32_t b = blockIdx.x;
+    if (n_slices < 8) {
+        slice = b / n_tiles;
+        tile = b % n_tiles;
+    } else {
+        slice = b / 8 / n_tiles * 8 + b % 8;
+        tile = b / 8 % n_tiles;
+    }
+    return slice < n_slices;
+}
+inline int grid_of(int32_t n_slices, int32_t n_tiles) {
+    return n_slices < 8 ? n_slices * n_tiles : (n_slices + 7) / 8 * 8 * n_tiles;
+}
+
+// Many rows: four waves of CX * 32 rows each share tiles of F through LDS, two
+// tiles deep (one is read while the next one's loads are in flight).
+template <int K, int NP, int CX, int YT, bool ENT>
+__global__ __launch_bounds__(kThreads, 2) void k_score_pass(ScoreK A) {
+    using TL = Tile<K, NP, YT>;
+    extern __shared__ __align__(16) unsigned char smem[];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, h = lane >> 5;
+    int32_t slice, tile;
+    if (!place(A.n_slices, A.n_tiles, slice, tile)) return;
+    const int64_t x0 = A.t0 + (int64_t)tile * (4 * CX * 32) + wave * (CX * 32);
+    const int64_t i0 = slice * A.slice_items, i1 = std::min<int64_t>(i0 + A.slice_items, A.F.count);
+    auto buf = [&](int b) { return reinterpret_cast<uint16_t *>(smem + b * TL::kBytes); };
+    if constexpr (K < 32) {
+        for (size_t j = threadIdx.x; j < 2 * TL::kBytes / 4; j += kThreads) reinterpret_cast<uint32_t *>(smem)[j] = 0u;
+        __syncthreads();
+    }
+    b8 x[CX][Shape<K, NP>::KS][NP];
+    const Side X{A.H.p, A.t0 + A.T, A.H.ld, nullptr};
+#pragma unroll
+    for (int q = 0; q < CX; ++q) load_x<K, NP>(X, x0 + 32 * q, A.turn, x[q]);
+    Stat st[CX];
+    TL t;
+    auto put = [&](uint16_t *b, int64_t y0) {
+        t.store(A.F, b);
+        if (threadIdx.x < YT) {
+            const int64_t i = y0 + threadIdx.x;
+            float o = kOff;
+            if (i < i1) {
+                o = A.F.bias ? A.F.bias[i] : 0.f;
+                o = o < kExcluded ? kOff : o * A.bias_c;
+            }
+            reinterpret_cast<float *>(b + NP * TL::kPlane)[threadIdx.x] = o;
+        }
+    };
+    int cur = 0;
+    t.load(A.F, i0);
+    put(buf(0), i0);
+    __syncthreads();
+    for (int64_t y0 = i0; y0 < i1; y0 += YT) {
+        const bool more = y0 + YT < i1;
+        if (more) t.load(A.F, y0 + YT);
+        const uint16_t *b = buf(cur);
+        const float *off = reinterpret_cast<const float *>(b + NP * TL::kPlane) + 4 * h;
+        const bool masked = A.F.bias || y0 + YT > i1;
+#pragma unroll
+        for (int u = 0; u < YT / 32; ++u) {
+            f16 acc[CX];
+#pragma unroll
+            for (int q = 0; q < CX; ++q) acc[q] = scores<K, NP, YT>(b + u * 32 * Shape<K, NP>::RS, x[q]);
+            float top[CX];
+            if (masked) {
+#pragma unroll
+                for (int q = 0; q < CX; ++q) top[q] = take<ENT, true>(st[q], acc[q], A.c, off + 32 * u);
+            } else {
+#pragma unroll
+                for (int q = 0; q < CX; ++q) top[q] = take<ENT, false>(st[q], acc[q], A.c, nullptr);
+            }
+            if (A.blkmax && y0 + 32 * u < i1) {
+#pragma unroll
+                for (int q = 0; q < CX; ++q) {
+                    const float v = fmaxf(top[q], __shfl_xor(top[q], 32, 64));
+                    const int64_t row = x0 - A.t0 + 32 * q + (lane & 31);
+                    if (h == 0 && row < A.T) A.blkmax[((y0 + 32 * u) >> 5) * A.T + row] = v;
+                }
+            }
+        }
+        if (more) put(buf(cur ^ 1), y0 + YT);
+        __syncthreads();
+        cur ^= 1;
+    }
+#pragma unroll
+    for (int q = 0; q < CX; ++q) {
+        Stat o{__shfl_xor(st[q].m, 32, 64), __shfl_xor(st[q].s, 32, 64), __shfl_xor(st[q].e, 32, 64)};
+        merge(st[q], o);
+        const int64_t row = x0 - A.t0 + 32 * q + (lane & 31);
+        if (h == 0 && row < A.T) A.part[(int64_t)slice * A.T + row] = make_float4(st[q].m, st[q].s, st[q].e, 0.f);
+    }
+}
+
+// At most 32 rows: reading F is all there is, so every wave takes blocks of 32
+// items of its own straight from memory into the A operand (a row's 128-byte
+// lines are read by two to four loads that follow one another).
+template <int K, int NP, bool ENT>
+__global__ __launch_bounds__(kThreads, 2) void k_score_few(ScoreK A) {
+    using S = Shape<K, NP>;
+    __shared__ float4 join[4][32];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, h = lane >> 5;
+    const int32_t slice = blockIdx.x;
+    const int64_t i0 = slice * A.slice_items, i1 = std::min<int64_t>(i0 + A.slice_items, A.F.count);
+    b8 x[S::KS][NP];
+    load_x<K, NP>(Side{A.H.p, A.t0 + A.T, A.H.ld, nullptr}, A.t0, A.turn, x);
+    Stat st;
+    for (int64_t y0 = i0 + wave * 32; y0 < i1; y0 += 128) {
+        const int64_t item = y0 + (lane & 31);
+        float o = kOff;
+        if (item < i1) {
+            o = A.F.bias ? A.F.bias[item] : 0.f;
+            o = o < kExcluded ? kOff : o * A.bias_c;
+        }
+        Raw<NP> raw[S::KS];
+#pragma unroll
+        for (int s = 0; s < S::KS; ++s) {
+            const int c = 16 * s + 8 * h;
+            raw[s] = zero_raw<NP>();
+            if (o != kOff && c < K) raw[s] = load_raw<NP>(A.F.p, item * A.F.ld + c);
+        }
+        f16 acc = {};
+#pragma unroll
+        for (int s = 0; s < S::KS; ++s) {
+            b8 a[NP];
+            parts_of<NP>(raw[s], a);
+            acc = product<NP>(a, x[s], acc);
+        }
+        float top;
+        if (A.F.bias || y0 + 32 > i1) {
+            __align__(16) float off[32];  // offsets of rows 4 h + 8 q + j at 8 q + j
+#pragma unroll
+            for (int r = 0; r < 16; ++r) off[tile_row(r)] = __shfl(o, tile_row(r) + 4 * h, 64);
+            top = take<ENT, true>(st, acc, A.c, off);
+        } else {
+            top = take<ENT, false>(st, acc, A.c, nullptr);
+        }
+        if (A.blkmax) {
+            const float v = fmaxf(top, __shfl_xor(top, 32, 64));
+            if (lane < A.T) A.blkmax[(y0 >> 5) * A.T + lane] = v;
+        }
+    }
+    Stat o{__shfl_xor(st.m, 32, 64), __shfl_xor(st.s, 32, 64), __shfl_xor(st.e, 32, 64)};
+    merge(st, o);
+    if (h == 0) join[wave][lane] = make_float4(st.m, st.s, st.e, 0.f);
+    __syncthreads();
+    if (threadIdx.x < A.T) {
+        Stat all{join[0][lane].x, join[0][lane].y, join[0][lane].z};
+        for (int w = 1; w < 4; ++w) merge(all, Stat{join[w][lane].x, join[w][lane].y, join[w][lane].z});
+        A.part[(int64_t)slice * A.T + lane] = make_float4(all.m, all.s, all.e, 0.f);
+    }
+}
+
+// sup[g][t] = the largest of blkmax[b][t] over the G blocks of group g.
+__global__ __launch_bounds__(kThreads) void k_block_groups(const float *blkmax, int64_t T, int64_t nblk, int64_t G,
+                                                           int64_t ngrp, float *sup) {
+    const int64_t j = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+    if (j >= ngrp * T) return;
+    const int64_t g = j / T, t = j % T;
+    const int64_t b1 = std::min<int64_t>((g + 1) * G, nblk);
+    float v = kOff;
+    for (int64_t b = g * G; b < b1; ++b) v = fmaxf(v, blkmax[b * T + t]);
+    sup[j] = v;
+}
+
+// ------------------------------------------------- a row's results
+
+constexpr int kMargin = 16;                     // blocks beyond the wanted best items that are looked at
+constexpr int kMaxPick = TSID_MAX_TOP + kMargin;
+constexpr int kSelCap = 4096;                   // candidates chosen from at a time
+constexpr int kMaxGroups = 2048;
+
+// Larger floats have larger keys; NaN is below everything.
+__device__ __forceinline__ uint32_t order_key(float v) {
+    if (!(v == v)) return 0u;
+    const uint32_t b = __float_as_uint(v);
+    return (b & 0x80000000u) ? ~b : b | 0x80000000u;
+}
+__device__ __forceinline__ uint64_t order_key(double v) {
+    if (!(v == v)) return 0ull;
+    const uint64_t b = __double_as_longlong(v);
+    return (b >> 63) ? ~b : b | (1ull << 63);
+}
+
+struct SelectLds {
+    uint32_t hist[256], wsum[4];
+    uint32_t digit, need, count;
+};
+
+// Sum over the threads before this one of the 256, and all of them.
+__device__ __forceinline__ uint32_t before(uint32_t v, uint32_t *wsum, uint32_t &total) {
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+    uint32_t incl = v;
+#pragma unroll
+    for (int off = 1; off < 64; off <<= 1) {
+        const uint32_t o = __shfl_up(incl, off, 64);
+        if (lane >= off) incl += o;
+    }
+    __syncthreads();
+    if (lane == 63) wsum[w] = incl;
+    __syncthreads();
+    uint32_t pre = 0;
+    total = 0;
+    for (int q = 0; q < 4; ++q) {
+        if (q < w) pre += wsum[q];
+        total += wsum[q];
+    }
+    return pre + incl - v;
+}
+
+// Places (ascending) of the `want` largest of key[0 .. N - 1] to place[0 ..];
+// equal keys: the first ones.  Digit by digit from the top, until the keys
+// that share the digits so far are all wanted.  Returns how many.
+template <typename U>
+__device__ int select_largest(const U *key, int N, int want, int32_t *place, SelectLds &L) {
+    const int t = threadIdx.x;
+    if (want >= N) {
+        for (int j = t; j < N; j += kThreads) place[j] = j;
+        __syncthreads();
+        return N;
+    }
+    U prefix = 0, mask = 0;
+    uint32_t need = (uint32_t)want;
+    bool all = false;
+    for (int shift = (int)sizeof(U) * 8 - 8; shift >= 0 && !all; shift -= 8) {
+        L.hist[t] = 0u;
+        __syncthreads();
+        for (int j = t; j < N; j += kThreads)
+            if ((key[j] & mask) == prefix) atomicAdd(&L.hist[(uint32_t)(key[j] >> shift) & 255u], 1u);
+        __syncthreads();
+        uint32_t total;
+        const uint32_t mine = L.hist[255 - t];  // thread t: digit 255 - t
+        const uint32_t above = before(mine, L.wsum, total);
+        if (above < need && need <= above + mine) {
+            L.digit = 255u - t;
+            L.need = need - above;
+            L.count = mine;
+        }
+        __syncthreads();
+        prefix |= (U)L.digit << shift;
+        mask |= (U)255u << shift;
+        need = L.need;
+        all = L.count == need;
+        __syncthreads();
+    }
+    const int per = (N + kThreads - 1) / kThreads, j0 = t * per, j1 = j0 + per < N ? j0 + per : N;
+    uint32_t eq = 0, total;
+    for (int j = j0; j < j1; ++j) eq += (key[j] & mask) == prefix;
+    uint32_t eq_before = before(eq, L.wsum, total), take = 0, e = eq_before;
+    for (int j = j0; j < j1; ++j) {
+        const U v = key[j] & mask;
+        take += v > prefix || (v == prefix && e++ < need);
+    }
+    uint32_t at = before(take, L.wsum, total);
+    e = eq_before;
+    for (int j = j0; j < j1; ++j) {
+        const U v = key[j] & mask;
+        if (v > prefix || (v == prefix && e++ < need)) place[at++] = j;
+    }
+    __syncthreads();
+    return (int)total;
+}
+
+struct FinishK {
+    const float4 *part;
+    int32_t n_parts;
+    Side H, F;
+    int32_t k;
+    double scale, bias_scale;
+    int64_t t0, T;
+    const int32_t *ids;
+    int32_t per_row;
+    float *lse, *logp, *entropy;
+    const float *teacher;  // distillation: loss from these
+    double tau;
+    float *loss;
+    int32_t top;
+    const float *blkmax, *sup;
+    int64_t nblk, G, ngrp;
+    int32_t *top_ids;
+    float *top_logp;
+    int32_t *err;
+};
+
+template <typename E>
+__device__ __forceinline__ double value(const E *p);
+template <>
+__device__ __forceinline__ double value(const float *p) { return (double)*p; }
+template <>
+__device__ __forceinline__ double value(const uint16_t *p) { return (double)__uint_as_float((uint32_t)*p << 16); }
+
+__device__ __forceinline__ double block_sum(double v, double *red) {
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1) v += __shfl_xor(v, off, 64);
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
+    __syncthreads();
+    return (red[0] + red[1]) + (red[2] + red[3]);
+}
+__device__ __forceinline__ float block_max(float v, double *red) {
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1) v = fmaxf(v, __shfl_xor(v, off, 64));
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = (double)v;
+    __syncthreads();
+    return (float)fmax(fmax(red[0], red[1]), fmax(red[2], red[3]));
+}
+
+// One workgroup per row: the slices' sums joined in fp64, the given items'
+// scores in fp64, and the best items.  The best `top` items lie in the `top`
+// blocks of 32 whose maxima are largest (an item outside them has `top` better
+// ones), so those blocks and kMargin more, for the rounding of the maxima, are
+// scored again in fp64 and the best are ranked by these scores.  The blocks are
+// found through groups of blocks in the same way.
+template <typename E>
+__global__ __launch_bounds__(kThreads) void k_score_finish(FinishK A) {
+    __shared__ double hrow[128], red[4];
+    __shared__ __align__(16) unsigned char cand[kSelCap * 8];
+    __shared__ int32_t pick[2][kMaxPick], place_[kMaxPick];
+    __shared__ SelectLds L;
+    const int tid = threadIdx.x;
+    const int64_t row = blockIdx.x, t = A.t0 + row;
+    const E *H = static_cast<const E *>(A.H.p), *F = static_cast<const E *>(A.F.p);
+    if (tid < A.k) hrow[tid] = value(H + t * A.H.ld + tid);
+    // log sum and entropy
+    float m = kLeast;
+    for (int q = tid; q < A.n_parts; q += kThreads) m = fmaxf(m, A.part[(int64_t)q * A.T + row].x);
+    m = block_max(m, red);
+    double s = 0.0, e = 0.0;
+    for (int q = tid; q < A.n_parts; q += kThreads) {
+        const float4 p = A.part[(int64_t)q * A.T + row];
+        if (p.y == 0.f) continue;
+        const double d = (double)p.x - (double)m, f = exp2(d);
+        s += (double)p.y * f;
+        e += ((double)p.z + (double)p.y * d) * f;
+    }
+    s = block_sum(s, red);
+    e = block_sum(e, red);
+    const bool empty = s == 0.0;
+    const double lse = empty ? -INFINITY : kLn2 * ((double)m + log2(s));
+    if (tid == 0) {
+        if (A.lse) A.lse[t] = (float)lse;
+        if (A.entropy) A.entropy[t] = empty ? 0.f : (float)(kLn2 * (log2(s) - e / s));
+    }
+    // the given items: 16 lanes each
+    const int sub = tid & 15;
+    auto usable = [&](int32_t id) { return id >= 0 && id < A.F.count && !(A.F.bias && A.F.bias[id] < kExcluded); };
+    auto logp_of = [&](int32_t id) {
+        double z = 0.0;
+        for (int c = sub; c < A.k; c += 16) z = fma(hrow[c], value(F + (int64_t)id * A.F.ld + c), z);
+#pragma unroll
+        for (int off = 8; off > 0; off >>= 1) z += __shfl_xor(z, off, 16);
+        return z * A.scale + (A.F.bias ? (double)A.F.bias[id] * A.bias_scale : 0.0) - lse;
+    };
+    const int32_t *ids = A.ids ? A.ids + t * A.per_row : nullptr;
+    if (A.logp) {
+        for (int j = tid >> 4; j < A.per_row; j += kThreads / 16) {
+            const int32_t id = ids[j];
+            float v = 0.f;
+            if (usable(id)) v = (float)logp_of(id);
+            else if (id >= 0 && id < A.F.count) v = -INFINITY;
+            else if (id != -1) A.err[ERR_RANGE] = 1;
+            if (sub == 0) A.logp[t * A.per_row + j] = v;
+        }
+    }
+    if (A.teacher) {
+        const float *tl = A.teacher + t * A.per_row;
+        float tm = -INFINITY;
+        for (int j = tid; j < A.per_row; j += kThreads) {
+            const int32_t id = ids[j];
+            if (usable(id)) tm = fmaxf(tm, tl[j]);
+            else if (id < -1 || id >= A.F.count) A.err[ERR_RANGE] = 1;
+        }
+        tm = block_max(tm, red);
+        double w_sum = 0.0, a_sum = 0.0;
+        if (tm > -INFINITY) {
+            for (int j = tid >> 4; j < A.per_row; j += kThreads / 16) {
+                if (!usable(ids[j])) continue;
+                const double lw = ((double)tl[j] - (double)tm) / A.tau, w = exp(lw);
+                const double lp = logp_of(ids[j]);
+                if (sub == 0 && w > 0.0) {
+                    w_sum += w;
+                    a_sum += w * (lw - lp);
+                }
+            }
+        }
+        w_sum = block_sum(w_sum, red);
+        a_sum = block_sum(a_sum, red);
+        if (tid == 0) A.loss[t] = w_sum > 0.0 ? (float)(A.tau * A.tau * (a_sum / w_sum - log(w_sum))) : 0.f;
+    }
+    if (A.top <= 0) return;
+    // the blocks that hold the best items
+    uint32_t *key = reinterpret_cast<uint32_t *>(cand);
+    int32_t *pay = reinterpret_cast<int32_t *>(cand + kSelCap * 4);
+    // the `want` largest of total candidates get(j) -> (value, payload), payloads ascending, to out
+    auto choose = [&](int64_t total, int want, int32_t *out, auto get) {
+        int have = 0;
+        int64_t next = 0;
+        do {
+            const int n_new = (int)std::min<int64_t>(kSelCap - have, total - next);
+            for (int j = tid; j < n_new; j += kThreads) {
+                float v;
+                int32_t p;
+                get(next + j, v, p);
+                key[have + j] = order_key(v);
+                pay[have + j] = p;
+            }
+            __syncthreads();
+            const int got = select_largest(key, have + n_new, want, place_, L);
+            next += n_new;
+            if (next < total) {  // keep them at the front for the next round
+                uint32_t k0 = 0;
+                int32_t p0 = 0;
+                if (tid < got) {
+                    k0 = key[place_[tid]];
+                    p0 = pay[place_[tid]];
+                }
+                __syncthreads();
+                if (tid < got) {
+                    key[tid] = k0;
+                    pay[tid] = p0;
+                }
+            } else {
+                if (tid < got) out[tid] = pay[place_[tid]];
+            }
+            have = got;
+            __syncthreads();
+        } while (next < total);
+        return have;
+    };
+    const int want = A.top + kMargin;
+    int got;
+    if (A.sup) {
+        const int groups = choose(A.ngrp, want, pick[0], [&](int64_t j, float &v, int32_t &p) {
+            v = A.sup[j * A.T + row];
+            p = (int32_t)j;
+        });
+        got = choose(groups * A.G, want, pick[1], [&](int64_t j, float &v, int32_t &p) {
+            const int64_t b = pick[0][j / A.G] * A.G + j % A.G;
+            v = b < A.nblk ? A.blkmax[b * A.T + row] : -INFINITY;
+            p = (int32_t)b;
+        });
+    } else {
+        got = choose(A.nblk, want, pick[1], [&](int64_t j, float &v, int32_t &p) {
+            v = A.blkmax[j * A.T + row];
+            p = (int32_t)j;
+        });
+    }
+    // their items in fp64, one lane per item
+    uint64_t *key64 = reinterpret_cast<uint64_t *>(cand);
+    for (int j = tid; j < got * 32; j += kThreads) {
+        const int64_t id = (int64_t)pick[1][j >> 5] * 32 + (j & 31);
+        uint64_t kv = 0ull;
+        if (id < A.F.count && usable((int32_t)id)) {
+            double z = 0.0;
+            const E *f = F + id * A.F.ld;
+#pragma unroll 8
+            for (int c = 0; c < A.k; ++c) z = fma(hrow[c], value(f + c), z);
+            z = z * A.scale + (A.F.bias ? (double)A.F.bias[id] * A.bias_scale : 0.0);
+            kv = order_key(z);
+        }
+        key64[j] = kv;
+    }
+    __syncthreads();
+    const int best = select_largest(key64, got * 32, A.top, place_, L);
+    if (tid < A.top) {
+        int32_t id = -1;
+        float lp = -INFINITY;
+        int rank = tid;
+        if (tid < best) {
+            const uint64_t kv = key64[place_[tid]];
+            rank = 0;
+            for (int j = 0; j < best; ++j) {
+                const uint64_t o = key64[place_[j]];
+                rank += o > kv || (o == kv && j < tid);
+            }
+            if (kv != 0ull) {
+                id = pick[1][place_[tid] >> 5] * 32 + (place_[tid] & 31);
+                const double z = __longlong_as_double((long long)((kv >> 63) ? kv & ~(1ull << 63) : ~kv));
+                lp = (float)(z - lse);
+            }
+        }
+        A.top_ids[t * A.top + rank] = id;
+        A.top_logp[t * A.top + rank] = lp;
+    }
+}
+
+// ------------------------------------------------------------- gradients
+
+// What a row's gradient in the scores needs (see HeadGrad): x = log2 of the
+// sum, y = a, z = b ln 2, corrected for x being rounded; and the weights of its
+// listed items.  One wave per row.
+__global__ __launch_bounds__(kThreads) void k_head_coef(HeadGrad G, int64_t T, int64_t n, const float *bias,
+                                                        float4 *coef, float *w, int32_t *err) {
+    const int64_t t = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (t >= T) return;
+    const int lane = threadIdx.x & 63;
+    const int32_t *ids = G.ids ? G.ids + t * G.per_row : nullptr;
+    const float lse = G.lse[t];
+    const bool empty = lse < -1e29f;
+    auto usable = [&](int32_t id) {
+        const bool in = id >= 0 && id < n;
+        if (!in && id != -1) err[ERR_RANGE] = 1;
+        return in && !empty && !(bias && bias[id] < kExcluded);
+    };
+    auto wave_sum = [](double v) {
+        for (int off = 32; off > 0; off >>= 1) v += __shfl_xor(v, off, 64);
+        return v;
+    };
+    double a = 0.0, b = 0.0;
+    if (G.teacher) {
+        const float *tl = G.teacher + t * G.per_row;
+        const double tau = G.temperature;
+        float tm = -INFINITY;
+        for (int j = lane; j < G.per_row; j += 64)
+            if (usable(ids[j])) tm = fmaxf(tm, tl[j]);
+        for (int off = 32; off > 0; off >>= 1) tm = fmaxf(tm, __shfl_xor(tm, off, 64));
+        double sum = 0.0;
+        for (int j = lane; j < G.per_row; j += 64)
+            if (usable(ids[j])) sum += exp(((double)tl[j] - (double)tm) / tau);
+        sum = wave_sum(sum);
+        const bool some = tm > -INFINITY;
+        const double u = some ? (double)G.dloss[t] * tau * tau : 0.0;
+        a = u;
+        for (int j = lane; j < G.per_row; j += 64)
+            w[t * G.per_row + j] =
+                some && usable(ids[j]) ? (float)(-u * exp(((double)tl[j] - (double)tm) / tau) / sum) : 0.f;
+    } else {
+        double sum = 0.0;
+        for (int j = lane; j < G.per_row; j += 64) {
+            const float v = usable(ids[j]) ? G.dlogp[t * G.per_row + j] : 0.f;
+            w[t * G.per_row + j] = v;
+            sum += (double)v;
+        }
+        sum = wave_sum(sum);
+        b = G.dentropy && !empty ? -(double)G.dentropy[t] : 0.0;
+        a = -sum + (b != 0.0 ? b * (double)G.entropy[t] : 0.0);
+    }
+    if (lane == 0) {
+        const double l2 = (double)lse * kLog2e;
+        const float l2f = (float)l2;
+        const double d = (double)l2f - l2, f = exp2(d);  // log2 p = (c s - l2f) + d
+        coef[t] = empty ? make_float4(-kLeast, 0.f, 0.f, 0.f)
+                        : make_float4(l2f, (float)(f * (a + b * kLn2 * d)), (float)(f * b * kLn2), 0.f);
+    }
+}
+
+struct GradK {
+    Side X, Y;
+    int32_t x_items;   // X holds the items (the gradient of F), Y the rows; else the other way round
+    float c;
+    int turn;
+    float bias_c;
+    const float4 *coef;
+    int64_t slice_rows;
+    int32_t n_slices, n_tiles;
+    float *part;       // [slice][rows of X][K]
+};
+
+// part[slice][x] = sum over the slice's rows y of g(x, y) y, with
+// g = p a + p log2 p b (ITEMS: a and b of the row y; else of the row x, where a
+// alone is left to the sum's end).  The scores leave 16 rows of Y in a lane,
+// eight at a time the A operand of the second product (its k index counts rows
+// of Y in the order the scores left them); the B operand is a column of the
+// same rows of the tile, by transposing LDS reads (ds_read_b64_tr_b16).  g is
+// rounded to bf16 for bf16 factors (2^-9 of a term of a sum that is itself
+// rounded to bf16), and split in three parts for fp32 ones.
+template <int K, int NP, int YT, bool ITEMS, bool ENT>
+__global__ __launch_bounds__(kThreads, 2) void k_grad_pass(GradK A) {
+    using S = Shape<K, NP>;
+    using TL = Tile<K, NP, YT>;
+    extern __shared__ __align__(16) unsigned char smem[];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, h = lane >> 5;
+    int32_t slice, tile;
+    if (!place(A.n_slices, A.n_tiles, slice, tile)) return;
+    const int64_t x0 = (int64_t)tile * 128 + wave * 32, xr = x0 + (lane & 31);
+    const int64_t i0 = slice * A.slice_rows, i1 = std::min<int64_t>(i0 + A.slice_rows, A.Y.count);
+    auto buf = [&](int b) { return reinterpret_cast<uint16_t *>(smem + b * TL::kBytes); };
+    if constexpr (K < 32) {
+        for (size_t j = threadIdx.x; j < 2 * TL::kBytes / 4; j += kThreads) reinterpret_cast<uint32_t *>(smem)[j] = 0u;
+        __syncthreads();
+    }
+    b8 x[S::KS][NP];
+    load_x<K, NP>(A.X, x0, A.turn, x);
+    // the lane's own part of the exponent's offset, and of the gradient
+    float own_off = 0.f, own_a = 0.f, own_b = 0.f;
+    if (xr < A.X.count) {
+        if constexpr (ITEMS) {
+            if (A.X.bias) own_off = A.X.bias[xr] < kExcluded ? kOff : A.X.bias[xr] * A.bias_c;
+        } else {
+            const float4 q = A.coef[xr];
+            own_off = -q.x;
+            own_a = q.y;
+            own_b = q.z;
+        }
+    }
+    f16 acc[S::NB] = {};
+    TL t;
+    // a row of Y: the offset; ITEMS: its a and b
+    auto put = [&](uint16_t *b, int64_t y0) {
+        t.store(A.Y, b);
+        if (threadIdx.x < YT) {
+            const int64_t i = y0 + threadIdx.x;
+            float *o = reinterpret_cast<float *>(b + NP * TL::kPlane) + threadIdx.x;
+            if constexpr (ITEMS) {
+                float4 q = make_float4(-kLeast, 0.f, 0.f, 0.f);
+                if (i < i1) q = A.coef[i];
+                o[0] = -q.x;
+                o[YT] = q.y;
+                o[2 * YT] = q.z;
+            } else {
+                float v = kOff;
+                if (i < i1) {
+                    v = A.Y.bias ? A.Y.bias[i] : 0.f;
+                    v = v < kExcluded ? kOff : v * A.bias_c;
+                }
+                o[0] = v;
+            }
+        }
+    };
+    const int grp = lane >> 4, gi = lane & 15;
+    int cur = 0;
+    t.load(A.Y, i0);
+    put(buf(0), i0);
+    __syncthreads();
+    for (int64_t y0 = i0; y0 < i1; y0 += YT) {
+        const bool more = y0 + YT < i1;
+        if (more) t.load(A.Y, y0 + YT);
+        const uint16_t *b = buf(cur);
+#pragma unroll
+        for (int u = 0; u < YT / 32; ++u) {
+            const uint16_t *yt = b + u * 32 * S::RS;
+            const float *off = reinterpret_cast<const float *>(b + NP * TL::kPlane) + 32 * u + 4 * h;
+            f16 g = scores<K, NP, YT>(yt, x);
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const f4 o = *reinterpret_cast<const f4 *>(off + 8 * q);
+                f4 ya = {}, yb = {};
+                if constexpr (ITEMS) {
+                    ya = *reinterpret_cast<const f4 *>(off + YT + 8 * q);
+                    if constexpr (ENT) yb = *reinterpret_cast<const f4 *>(off + 2 * YT + 8 * q);
+                }
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const float e = fmaf(g[4 * q + j], A.c, o[j] + own_off);
+                    const float p = __builtin_amdgcn_exp2f(e);
+                    if constexpr (ITEMS) g[4 * q + j] = p * (ENT ? fmaf(e, yb[j], ya[j]) : ya[j]);
+                    else g[4 * q + j] = ENT ? p * fmaf(e, own_b, own_a) : p;
+                }
+            }
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+                const f8 gs = {g[8 * s], g[8 * s + 1], g[8 * s + 2], g[8 * s + 3],
+                               g[8 * s + 4], g[8 * s + 5], g[8 * s + 6], g[8 * s + 7]};
+                b8 ga[NP];
+                if constexpr (NP == 1) ga[0] = __builtin_convertvector(gs, b8);
+                else split3(gs, ga);
+#pragma unroll
+                for (int nb = 0; nb < S::NB; ++nb) {
+                    // in each group of 16 lanes, lane i receives element i % 4
+                    // of the 8-byte pieces of lanes i / 4, 4 + i / 4, ...: lane
+                    // 4 j + q points at row j, coordinates 4 q .. 4 q + 3
+                    const uint16_t *src = yt + (16 * s + 4 * h + (gi >> 2)) * S::RS + nb * 32 + (grp & 1) * 16 + 4 * (gi & 3);
+                    b8 yb[NP];
+#pragma unroll
+                    for (int p = 0; p < NP; ++p) {
+                        const uint16_t *at = src + p * TL::kPlane;
+                        const uint2 lo = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                                                                       (__attribute__((address_space(3))) s4 *)(at)));
+                        const uint2 hi = __builtin_bit_cast(
+                            uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                                       (__attribute__((address_space(3))) s4 *)(at + 8 * S::RS)));
+                        yb[p] = __builtin_bit_cast(b8, make_uint4(lo.x, lo.y, hi.x, hi.y));
+                    }
+                    acc[nb] = product<NP>(ga, yb, acc[nb]);
+                }
+            }
+        }
+        if (more) put(buf(cur ^ 1), y0 + YT);
+        __syncthreads();
+        cur ^= 1;
+    }
+#pragma unroll
+    for (int nb = 0; nb < S::NB; ++nb) {
+        const int c = nb * 32 + (lane & 31);
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            const int64_t row = x0 + tile_row(r) + 4 * h;
+            if (row < A.X.count && c < K) A.part[((int64_t)slice * A.X.count + row) * K + c] = acc[nb][r];
+        }
+    }
+}
+
+// out[t] = scale (a_t * sum of the parts + sum_j w_tj F[id_tj]) (a_t in the parts already: coef null).
+template <typename E>
+__global__ __launch_bounds__(kThreads) void k_grad_rows(const float *part, int32_t n_parts, int64_t T, int k,
+                                                        const float4 *coef, const int32_t *ids, const float *w,
+                                                        int32_t per_row, const E *F, int64_t ldf, float scale, E *out,
+                                                        int64_t ldo) {
+    const int64_t j = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+    const int64_t t = j / (k / 4);
+    const int c = (int)(j % (k / 4)) * 4;
+    if (t >= T) return;
+    f4 sum = {};
+    for (int32_t p = 0; p < n_parts; ++p) sum += *reinterpret_cast<const f4 *>(part + ((int64_t)p * T + t) * k + c);
+    if (coef) sum *= coef[t].y;
+    f4 more = {};
+    for (int32_t q = 0; q < per_row; ++q) {
+        const float v = w[t * per_row + q];
+        if (v == 0.f) continue;  // also the entries that are no item's
+        const E *f = F + (int64_t)ids[t * per_row + q] * ldf + c;
+#pragma unroll
+        for (int x = 0; x < 4; ++x) more[x] = fmaf(v, (float)value(f + x), more[x]);
+    }
+    sum = (sum + more) * scale;
+    if constexpr (sizeof(E) == 4) {
+        *reinterpret_cast<f4 *>(out + t * ldo + c) = sum;
+    } else {
+        typedef __bf16 b4 __attribute__((ext_vector_type(4)));
+        *reinterpret_cast<uint2 *>(out + t * ldo + c) = __builtin_bit_cast(uint2, __builtin_convertvector(sum, b4));
+    }
+}
+
+// ------------------------------------------------------------- host side
+
+constexpr int kCus = 256;
+
+// Slices of a streamed side: about `wanted` workgroups in all, slices of at
+// least `least` rows and whole tiles; a multiple of the 8 XCDs from 8 on.
+void slices_of(int64_t rows, int64_t tiles, int64_t wanted, int64_t least, int64_t unit, int32_t &n_slices,
+               int64_t &slice_rows) {
+    int64_t ns = std::max<int64_t>(1, (wanted + tiles - 1) / std::max<int64_t>(tiles, 1));
+    ns = std::min<int64_t>(ns, std::max<int64_t>(1, rows / least));
+    if (ns >= 8) ns = ns / 8 * 8;
+    slice_rows = ((rows + ns - 1) / ns + unit - 1) / unit * unit;
+    slice_rows = std::max<int64_t>(slice_rows, unit);
+    n_slices = (int32_t)std::max<int64_t>(1, (rows + slice_rows - 1) / slice_rows);
+}
+
+struct ScorePlan {
+    bool few;
+    int64_t chunk;        // rows of a run
+    int64_t nblk, G, ngrp;
+    int32_t n_slices, n_tiles, cx;
+    int64_t slice_items;
+    float4 *part;
+    float *blkmax, *sup;
+};
+
+ScorePlan plan_score(int64_t T, int64_t n, int prec, int top, Carve &c) {
+    ScorePlan p{};
+    p.nblk = (n + 31) / 32;
+    p.few = T <= 32;
+    p.chunk = T;
+    if (top > 0) {  // at most 1 GiB of block maxima at a time
+        const int64_t most = std::max<int64_t>(256, (int64_t(1) << 28) / std::max<int64_t>(p.nblk, 1) / 256 * 256);
+        p.chunk = std::min(T, most);
+    }
+    p.cx = prec == TSID_BF16 ? 2 : 1;
+    if (p.few) {
+        p.n_tiles = 1;
+        slices_of(n, 1, 2 * kCus, 128, 128, p.n_slices, p.slice_items);
+    } else {
+        const int64_t rows = 128 * p.cx;
+        p.n_tiles = (int32_t)((p.chunk + rows - 1) / rows);
+        slices_of(n, p.n_tiles, 4 * kCus, 256, 64, p.n_slices, p.slice_items);
+    }
+    p.part = c.take<float4>((int64_t)p.n_slices * p.chunk);
+    if (top > 0) {
+        p.blkmax = c.take<float>(p.nblk * p.chunk);
+        if (p.nblk > kMaxGroups) {
+            p.G = (p.nblk + kMaxGroups - 1) / kMaxGroups;
+            p.ngrp = (p.nblk + p.G - 1) / p.G;
+            p.sup = c.take<float>(p.ngrp * p.chunk);
+        }
+    }
+    return p;
+}
+
+template <int K, int NP, bool ENT>
+void launch_score(const ScoreK &a, const ScorePlan &p, hipStream_t s) {
+    if (p.few) {
+        k_score_few<K, NP, ENT><<<p.n_slices, kThreads, 0, s>>>(a);
+    } else {
+        constexpr int CX = NP == 1 ? 2 : 1, YT = NP == 1 ? 64 : 32;
+        constexpr size_t lds = 2 * Tile<K, NP, YT>::kBytes;
+        static_assert(lds <= 64 * 1024, "within the default limit of dynamic LDS");
+        k_score_pass<K, NP, CX, YT, ENT><<<grid_of(p.n_slices, a.n_tiles), kThreads, lds, s>>>(a);
+    }
+    TSID_HIP(hipGetLastError());
+}
+
+template <int K, int NP>
+void launch_grad(bool items, bool ent, const GradK &a, hipStream_t s) {
+    constexpr int YT = NP == 1 ? 64 : 32;
+    constexpr size_t lds = 2 * Tile<K, NP, YT>::kBytes;
+    static_assert(lds <= 64 * 1024, "within the default limit of dynamic LDS");
+    const int grid = grid_of(a.n_slices, a.n_tiles);
+    if (items) {
+        if (ent) k_grad_pass<K, NP, YT, true, true><<<grid, kThreads, lds, s>>>(a);
+        else k_grad_pass<K, NP, YT, true, false><<<grid, kThreads, lds, s>>>(a);
+    } else {
+        if (ent) k_grad_pass<K, NP, YT, false, true><<<grid, kThreads, lds, s>>>(a);
+        else k_grad_pass<K, NP, YT, false, false><<<grid, kThreads, lds, s>>>(a);
+    }
+    TSID_HIP(hipGetLastError());
+}
+
+// f.template operator()<K, NP>() for the rank and precision at hand.
+template <typename Fn>
+void for_rank(int k, int prec, Fn &&f) {
+    auto np = [&](auto kk) {
+        if (prec == TSID_BF16) f(kk, std::integral_constant<int, 1>());
+        else f(kk, std::integral_constant<int, 3>());
+    };
+    switch (k) {
+        case 8: np(std::integral_constant<int, 8>()); break;
+        case 16: np(std::integral_constant<int, 16>()); break;
+        case 32: np(std::integral_constant<int, 32>()); break;
+        case 64: np(std::integral_constant<int, 64>()); break;
+        case 128: np(std::integral_constant<int, 128>()); break;
+        default: fail(TSID_E_INVAL, "unsupported rank");
+    }
+}
+
+Side side_of(const Rows &r, const float *bias) { return Side{r.p, r.count, r.ld, bias}; }
+
+// The pass over all items and the rows' results, a run of rows at a time.
+void score_rows(const Head &h, const ScorePlan &p, FinishK f, bool entropy, hipStream_t s) {
+    ScoreK a{};
+    a.H = side_of(h.H, nullptr);
+    a.F = side_of(h.F, h.bias);
+    a.c = (float)(std::fabs((double)h.scale) * kLog2e);
+    a.turn = h.scale < 0.f;
+    a.bias_c = (float)((double)h.bias_scale * kLog2e);
+    a.slice_items = p.slice_items;
+    a.n_slices = p.n_slices;
+    a.part = p.part;
+    a.blkmax = p.blkmax;
+    f.part = p.part;
+    f.n_parts = p.n_slices;
+    f.H = a.H;
+    f.F = a.F;
+    f.k = h.k;
+    f.scale = h.scale;
+    f.bias_scale = h.bias_scale;
+    f.blkmax = p.blkmax;
+    f.sup = p.sup;
+    f.nblk = p.nblk;
+    f.G = p.G;
+    f.ngrp = p.ngrp;
+    for (int64_t t0 = 0; t0 < h.H.count; t0 += p.chunk) {
+        a.t0 = f.t0 = t0;
+        a.T = f.T = std::min<int64_t>(p.chunk, h.H.count - t0);
+        a.n_tiles = (int32_t)((a.T + 128 * p.cx - 1) / (128 * p.cx));
+        for_rank(h.k, h.prec, [&](auto kk, auto np) {
+            if (entropy) launch_score<kk(), np(), true>(a, p, s);
+            else launch_score<kk(), np(), false>(a, p, s);
+        });
+        if (p.sup) {
+            k_block_groups<<<ceil_div(p.ngrp * a.T, kThreads), kThreads, 0, s>>>(p.blkmax, a.T, p.nblk, p.G, p.ngrp,
+                                                                                p.sup);
+            TSID_HIP(hipGetLastError());
+        }
+        if (h.prec == TSID_BF16) k_score_finish<uint16_t><<<(unsigned)a.T, kThreads, 0, s>>>(f);
+        else k_score_finish<float><<<(unsigned)a.T, kThreads, 0, s>>>(f);
+        TSID_HIP(hipGetLastError());
+    }
+}
+
+struct GradPlan {
+    int32_t h_slices, h_tiles, f_slices, f_tiles;
+    int64_t h_rows, f_rows;
+    float4 *coef;
+    float *w, *part;
+    SumPlan sum;
+};
+
+GradPlan plan_grad(int64_t T, int64_t n, int k, int per_row, Carve &c) {
+    GradPlan p{};
+    p.h_tiles = (int32_t)((T + 127) / 128);
+    p.f_tiles = (int32_t)((n + 127) / 128);
+    slices_of(n, p.h_tiles, 4 * kCus, 256, 64, p.h_slices, p.h_rows);
+    slices_of(T, p.f_tiles, 4 * kCus, 256, 64, p.f_slices, p.f_rows);
+    p.coef = c.take<float4>(T);
+    p.w = c.take<float>(T * per_row);
+    // the two sides take turns at the same parts
+    p.part = c.take<float>(std::max<int64_t>((int64_t)p.h_slices * T, (int64_t)p.f_slices * n) * k);
+    p.sum.entries = T * per_row;
+    p.sum.n = n;
+    p.sum.k = k;
+    carve_sum(p.sum, c);
+    return p;
+}
+
+}  // namespace
+
+size_t score_workspace(int64_t T, int64_t n, int k, int prec, int top) {
+    Carve c;
+    plan_score(T, n, prec, top, c);
+    return c.used;
+}
+
+void run_score(const Head &h, const ScoreOut &o, void *ws, int32_t *err, hipStream_t s) {
+    if (h.H.count <= 0) return;
+    Carve c{static_cast<char *>(ws)};
+    const ScorePlan p = plan_score(h.H.count, h.F.count, h.prec, o.top, c);
+    FinishK f{};
+    f.ids = o.ids;
+    f.per_row = o.per_row;
+    f.lse = o.lse;
+    f.logp = o.logp;
+    f.entropy = o.entropy;
+    f.top = o.top;
+    f.top_ids = o.top_ids;
+    f.top_logp = o.top_logp;
+    f.err = err;
+    score_rows(h, p, f, o.entropy != nullptr, s);
+}
+
+void run_distill(const Head &h, const DistillOut &o, void *ws, int32_t *err, hipStream_t s) {
+    if (h.H.count <= 0) return;
+    Carve c{static_cast<char *>(ws)};
+    const ScorePlan p = plan_score(h.H.count, h.F.count, h.prec, 0, c);
+    FinishK f{};
+    f.ids = o.ids;
+    f.per_row = o.per_row;
+    f.lse = o.lse;
+    f.teacher = o.teacher;
+    f.tau = o.temperature;
+    f.loss = o.loss;
+    f.err = err;
+    score_rows(h, p, f, false, s);
+}
+
+size_t head_grad_workspace(int64_t T, int64_t n, int k, int prec, int per_row) {
+    Carve c;
+    plan_grad(T, n, k, per_row, c);
+    return c.used;
+}
+
+void run_head_grad(const Head &h, const HeadGrad &g, void *ws, int32_t *err, hipStream_t s) {
+    const int64_t T = h.H.count, n = h.F.count;
+    Carve c{static_cast<char *>(ws)};
+    GradPlan p = plan_grad(T, n, h.k, g.per_row, c);
+    const bool ent = g.dentropy != nullptr;
+    if (T > 0) {
+        k_head_coef<<<ceil_div(T, 4), kThreads, 0, s>>>(g, T, n, h.bias, p.coef, p.w, err);
+        TSID_HIP(hipGetLastError());
+    }
+    GradK a{};
+    a.c = (float)(std::fabs((double)h.scale) * kLog2e);
+    a.turn = h.scale < 0.f;
+    a.bias_c = (float)((double)h.bias_scale * kLog2e);
+    a.coef = p.coef;
+    a.part = p.part;
+    if (g.dH.p && T > 0) {
+        a.X = side_of(h.H, nullptr);
+        a.Y = side_of(h.F, h.bias);
+        a.slice_rows = p.h_rows;
+        a.n_slices = p.h_slices;
+        a.n_tiles = p.h_tiles;
+        for_rank(h.k, h.prec, [&](auto kk, auto np) { launch_grad<kk(), np()>(false, ent, a, s); });
+        const int blocks = ceil_div(T * (h.k / 4), kThreads);
+        const float4 *coef = ent ? nullptr : p.coef;
+        if (h.prec == TSID_BF16)
+            k_grad_rows<uint16_t><<<blocks, kThreads, 0, s>>>(p.part, p.h_slices, T, h.k, coef, g.ids, p.w, g.per_row,
+                                                              static_cast<const uint16_t *>(h.F.p), h.F.ld, h.scale,
+                                                              static_cast<uint16_t *>(g.dH.p), g.dH.ld);
+        else
+            k_grad_rows<float><<<blocks, kThreads, 0, s>>>(p.part, p.h_slices, T, h.k, coef, g.ids, p.w, g.per_row,
+                                                           static_cast<const float *>(h.F.p), h.F.ld, h.scale,
+                                                           static_cast<float *>(g.dH.p), g.dH.ld);
+        TSID_HIP(hipGetLastError());
+    }
+    if (g.dF.p && n > 0) {
+        if (T > 0) {
+            a.X = side_of(h.F, h.bias);
+            a.Y = side_of(h.H, nullptr);
+            a.slice_rows = p.f_rows;
+            a.n_slices = p.f_slices;
+            a.n_tiles = p.f_tiles;
+            for_rank(h.k, h.prec, [&](auto kk, auto np) { launch_grad<kk(), np()>(true, ent, a, s); });
+        }
+        launch_sum_sort(p.sum, g.ids, h.bias, err, s);
+        SumArgs sa{};
+        sa.X = h.H;
+        sa.w = p.w;
+        sa.per_row = std::max(1, g.per_row);
+        sa.parts = p.part;
+        sa.n_parts = T > 0 ? p.f_slices : 0;
+        sa.part_stride = n * h.k;
+        sa.scale = h.scale;
+        sa.out = g.dF;
+        launch_sum_rows(p.sum, h.prec, sa, s);
+    }
+}
+
+}  // namespace tsid

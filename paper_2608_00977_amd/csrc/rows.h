@@ -1,0 +1,118 @@
+// Operators on rows of factor tables (rows.hip) and on the probabilities that
+// factors give over all items (head.hip).  Internal; the entry points are in
+// include/tsid.h.
+#pragma once
+
+#include "internal.h"
+
+namespace tsid {
+
+// Takes pieces of a caller's workspace, each 256-byte aligned; with a null
+// base it only counts, so that the sizes asked for and the pieces taken come
+// from the same code.
+struct Carve {
+    char *base = nullptr;
+    size_t used = 0;
+    template <typename T>
+    T *take(int64_t count) {
+        T *p = base ? reinterpret_cast<T *>(base + used) : nullptr;
+        used += ((size_t)(count > 0 ? count : 1) * sizeof(T) + 255) & ~size_t(255);
+        return p;
+    }
+};
+
+// Rows of a factor table: fp32 or bf16, k per row, ld elements from row to row.
+struct Rows {
+    void *p;
+    int64_t count, ld;
+};
+
+// out[t] = scale * F[ids[t]]; id -1 gives zeros, another id outside the table
+// zeros and ERR_RANGE.
+void launch_lookup(int k, int prec, const Rows &F, const int32_t *ids, float scale, const Rows &out, int32_t *err,
+                   hipStream_t s);
+
+// Sums of weighted rows by id: entry e (0 .. entries - 1) adds w[e] times row
+// e / per_row of X to the sum of row ids[e].  Used as the gradient of a lookup
+// (w null, per_row 1) and for the listed items' part of a table's gradient.
+struct SumPlan {
+    int64_t entries, n;
+    int k;
+    // pieces of the workspace
+    uint64_t *keys[2];
+    uint32_t *vals[2];
+    uint32_t *sort_scratch;
+    uint32_t *ptr;       // n + 1: first sorted entry of each row
+    float *carry[2];     // sums of pieces of long rows, two per piece (two levels)
+    bool alt;            // where the sort left its result
+};
+// Entries one piece of a long row's sum takes, and the row length from which
+// a row is summed in pieces.
+constexpr int kSumPiece = 64;
+void carve_sum(SumPlan &p, Carve &c);
+// Sorts the entries by id (entries whose id is not in [0, n), or whose row of
+// the table is excluded by bias, go last and add nothing; ids other than -1
+// outside the table set ERR_RANGE).
+void launch_sum_sort(SumPlan &p, const int32_t *ids, const float *bias, int32_t *err, hipStream_t s);
+// out[i] = scale * (sum of the entries of i + sum of the parts' rows i), every
+// row of out written; parts: n_parts fp32 arrays of n x k, part_stride apart.
+struct SumArgs {
+    Rows X;
+    const float *w;
+    int32_t per_row;
+    const float *parts;
+    int32_t n_parts;
+    int64_t part_stride;
+    float scale;
+    Rows out;
+};
+void launch_sum_rows(const SumPlan &p, int prec, const SumArgs &a, hipStream_t s);
+
+// ------------------------------------------------------------------- head
+// Scores z_ti = scale h_t . f_i + bias_i of all items for all rows, divided by
+// the temperature.
+struct Head {
+    Rows H, F;
+    const float *bias;
+    int k, prec;
+    float scale;    // already divided by the temperature
+    float bias_scale;  // 1 / temperature
+};
+// A bias below this excludes its item: its row of F is never used.
+constexpr float kExcluded = -1e20f;
+
+struct ScoreOut {
+    const int32_t *ids;
+    int32_t per_row, top;
+    float *lse, *logp, *entropy;
+    int32_t *top_ids;
+    float *top_logp;
+};
+size_t score_workspace(int64_t T, int64_t n, int k, int prec, int top);
+void run_score(const Head &h, const ScoreOut &o, void *ws, int32_t *err, hipStream_t s);
+
+// dz_ti = (a_t + b_t log p_ti) p_ti + sum_j c_tj [i = id_tj].
+struct HeadGrad {
+    const int32_t *ids;
+    int32_t per_row;
+    const float *lse;
+    // of log probabilities and entropy
+    const float *dlogp, *entropy, *dentropy;
+    // of a distillation
+    const float *teacher, *dloss;
+    float temperature;
+    Rows dH, dF;  // p null: not wanted
+};
+size_t head_grad_workspace(int64_t T, int64_t n, int k, int prec, int per_row);
+void run_head_grad(const Head &h, const HeadGrad &g, void *ws, int32_t *err, hipStream_t s);
+
+struct DistillOut {
+    const int32_t *ids;
+    int32_t per_row;
+    const float *teacher;
+    float temperature;
+    float *loss, *lse;
+};
+void run_distill(const Head &h, const DistillOut &o, void *ws, int32_t *err, hipStream_t s);
+
+}  // namespace tsid

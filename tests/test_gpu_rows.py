@@ -1,0 +1,573 @@
+"""The row operators (lookup, scores over all items, distillation, and their gradients) against their
+definitions in 64 bits (rows_ref.py, which also derives every tolerance), at the sizes, types, masks, strides
+and ids where they can go wrong."""
+import numpy as np
+import pytest
+
+import rows_ref as ref
+from gpu_util import note
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def X():
+    import paper_2608_00977_amd as tsid
+    t = tsid.Tsid(0)
+    yield t
+    t.close()
+
+
+def _dtype(prec):
+    import torch
+    return torch.bfloat16 if prec == "bf16" else torch.float32
+
+
+def _table(g, rows, k, prec, size=1.0, ld=None):
+    """A factor table on the GPU (row stride ld), and its values in 64 bits."""
+    import torch
+    full = torch.from_numpy((size * g.standard_normal((rows, ld or k))).astype(np.float32)).to(_dtype(prec)).cuda()
+    view = full[:, :k]
+    return view, view.double().cpu().numpy()
+
+
+def _gpu(a, dtype=np.float32):
+    import torch
+    return torch.from_numpy(np.ascontiguousarray(a, dtype)).cuda()
+
+
+def _near(got, want, bound, what):
+    got = got.double().cpu().numpy() if hasattr(got, "cpu") else got
+    want, bound = np.asarray(want, np.float64), np.broadcast_to(bound, np.shape(want))
+    assert got.shape == want.shape, what
+    inf = ~np.isfinite(want)
+    assert np.array_equal(got[inf], want[inf]), what
+    off = np.abs(got[~inf] - want[~inf])
+    worst = off - bound[~inf]
+    assert off.size == 0 or worst.max() <= 0, (what, float(off.max()), float(bound[~inf][worst.argmax()]))
+
+
+# ------------------------------------------------------------------ lookup
+
+@pytest.mark.parametrize("prec", ["fp32", "bf16"])
+@pytest.mark.parametrize("k", [8, 16, 32, 64, 128])
+@pytest.mark.parametrize("count,n,ld", [(1, 1, 0), (7, 3, 8), (1025, 100, 0), (4099, 30011, 16)])
+def test_lookup_is_the_scaled_row(X, prec, k, count, n, ld):
+    import torch
+    g = np.random.default_rng(count + k)
+    F, _ = _table(g, n, k, prec, ld=k + ld)
+    ids = g.integers(-1, n, count)
+    note(f"lookup {prec} k={k} count={count} n={n}")
+    out = X.lookup(F, _gpu(ids, np.int32), scale=-1.7)
+    rows = F.float().cpu()[torch.from_numpy(np.maximum(ids, 0))] * torch.tensor(-1.7, dtype=torch.float32)
+    rows[torch.from_numpy(ids < 0)] = 0
+    assert torch.equal(out.cpu(), rows.to(F.dtype))
+    X.rows_check()
+
+
+@pytest.mark.parametrize("prec", ["fp32", "bf16"])
+@pytest.mark.parametrize("k,count,n", [(8, 0, 5), (8, 1, 1), (16, 64, 1), (32, 65, 1), (64, 129, 2), (128, 300, 7),
+                                       (32, 5000, 3), (64, 9001, 1), (128, 70001, 100), (8, 300000, 11),
+                                       (64, 500, 8192), (16, 100003, 50021)])
+def test_lookup_grad_sums_equal_ids(X, prec, k, count, n):
+    import torch
+    g = np.random.default_rng(count + n)
+    G, Gd = _table(g, count, k, prec, ld=k + 8)
+    ids = np.where(g.random(count) < 0.5, g.integers(-1, n, count), np.minimum(g.integers(0, 3, count), n - 1))
+    ids = np.where(g.random(count) < 0.05, -1, ids)
+    note(f"lookup_grad {prec} k={k} count={count} n={n}")
+    out = X.lookup_grad(G, _gpu(ids, np.int32), n, scale=0.3)
+    want, size = np.zeros((n, k)), np.zeros((n, k))
+    np.add.at(want, ids[ids >= 0], Gd[ids >= 0])
+    np.add.at(size, ids[ids >= 0], np.abs(Gd[ids >= 0]))
+    s = float(np.float32(0.3))
+    # a sum of pieces of 64 of pieces of 64: at most 64 + 64 + count / 4096 additions on one way
+    adds = min(count, 130 + count // 4096)
+    bound = adds * ref.U * s * size + 2 * ref.U * s * np.abs(want) + (ref.V * s * np.abs(want) if prec == "bf16" else 0)
+    _near(out, s * want, bound * 1.01, "lookup_grad")
+    assert torch.equal(out, X.lookup_grad(G, _gpu(ids, np.int32), n, scale=0.3))  # the same bits
+
+
+def test_lookup_grad_writes_every_row_of_a_strided_output_and_nothing_else(X):
+    import torch
+    full = torch.full((50, 40), 7.0, device="cuda")
+    G = torch.ones((3, 32), device="cuda")
+    X.lookup_grad(G, _gpu([4, 4, 9], np.int32), 20, out=full[:20, :32])
+    want = torch.full((50, 40), 7.0)
+    want[:20, :32] = 0
+    want[4, :32], want[9, :32] = 2, 1
+    assert torch.equal(full.cpu(), want)
+
+
+def test_ids_out_of_range_are_reported_once_and_skipped(X):
+    import torch
+    import paper_2608_00977_amd as tsid
+    F = torch.ones((10, 8), device="cuda")
+    for bad in (10, -2, 2 ** 31 - 1, -2 ** 31):
+        out = X.lookup(F, _gpu([0, bad, 9], np.int32))
+        assert out.cpu().sum(1).tolist() == [8.0, 0.0, 8.0]
+        with pytest.raises(tsid.TsidError) as e:
+            X.rows_check()
+        assert e.value.status == 2
+        X.rows_check()
+        d = X.lookup_grad(torch.ones((3, 8), device="cuda"), _gpu([1, bad, 1], np.int32), 10)
+        assert d.cpu()[:, 0].tolist() == [0, 2, 0, 0, 0, 0, 0, 0, 0, 0]
+        with pytest.raises(tsid.TsidError):
+            X.rows_check()
+        r = X.score(F[:2], F, ids=_gpu([[1, bad], [bad, 3]], np.int32))
+        assert r.logp.cpu()[0, 1] == 0 and r.logp.cpu()[1, 0] == 0
+        with pytest.raises(tsid.TsidError):
+            X.rows_check()
+        loss, lse = X.distill(F[:2], F, _gpu([[1, bad], [bad, 3]], np.int32), torch.zeros((2, 2), device="cuda"))
+        X.distill_grad(F[:2], F, _gpu([[1, bad], [bad, 3]], np.int32), torch.zeros((2, 2), device="cuda"), lse,
+                       torch.ones(2, device="cuda"))
+        assert np.allclose(loss.cpu().numpy(), np.log(10.0), atol=1e-5)
+        with pytest.raises(tsid.TsidError):
+            X.rows_check()
+
+
+# ------------------------------------------------------------------- scores
+
+SIZES = [(1, 1), (1, 33), (3, 31), (32, 64), (31, 4097), (33, 100), (129, 65), (257, 1000), (64, 2500)]
+
+
+def _problem(seed, T, n, k, prec, bias, m, ld=0):
+    """bias: None, "some" (a bias, some items excluded, whose rows hold NaN and infinities), "all" excluded."""
+    import torch
+    g = np.random.default_rng(seed)
+    H, Hd = _table(g, T, k, prec, ld=k + ld)
+    F, Fd = _table(g, n, k, prec, ld=k + ld)
+    b = None
+    if bias is not None:
+        b = g.normal(0, 1, n).astype(np.float32)
+        out = g.random(n) < (0.2 if bias == "some" else 2.0)
+        b[out] = g.choice(np.array([-np.inf, np.finfo(np.float32).min, -1.1e20], np.float32), int(out.sum()))
+        F[torch.from_numpy(out).cuda()] = _gpu(g.choice(np.array([np.nan, np.inf, -np.inf, 1e30], np.float32),
+                                                        (int(out.sum()), k))).to(F.dtype)
+        Fd[out] = 0.0
+    ids = g.integers(-1, n, (T, m))
+    if m > 2:
+        ids[:, 2] = ids[:, 0]  # the same item twice
+    return g, H, Hd, F, Fd, b, ids
+
+
+def _check_score(X, prob, prec, scale, top, n, T):
+    g, H, Hd, F, Fd, b, ids = prob
+    r = X.score(H, F, ids=_gpu(ids, np.int32), scale=scale, bias=None if b is None else _gpu(b), top=top, entropy=True)
+    X.rows_check()
+    w = ref.score(Hd, Fd, ids, float(np.float32(scale)), b, top)
+    out = np.zeros(n, bool) if b is None else b < ref.EXCLUDED
+    zb = ref.z_bound(Hd, Fd, out, scale, 1.0, b)
+    lb = ref.lse_bound(zb, w["lse"], n)
+    _near(r.lse, w["lse"], lb, "lse")
+    _near(r.logp, w["logp"], lb[:, None] + 2 * ref.U * np.abs(np.where(np.isfinite(w["logp"]), w["logp"], 0)), "logp")
+    _near(r.entropy, w["entropy"], ref.entropy_bound(zb, w["entropy"], n), "entropy")
+    assert np.array_equal(r.top_ids.cpu().numpy(), w["top_ids"])
+    _near(r.top_logp, w["top_logp"], lb[:, None] + 2 * ref.U * np.abs(np.where(np.isfinite(w["top_logp"]), w["top_logp"], 0)),
+          "top_logp")
+    return r
+
+
+@pytest.mark.parametrize("prec", ["fp32", "bf16"])
+@pytest.mark.parametrize("bias", [None, "some"])
+@pytest.mark.parametrize("T,n", SIZES)
+def test_score(X, prec, bias, T, n):
+    k = [8, 16, 32, 64, 128][(T + n) % 5]
+    note(f"score {prec} T={T} n={n} k={k} bias={bias}")
+    _check_score(X, _problem(T * 7 + n, T, n, k, prec, bias, 3, ld=8 if n % 2 else 0), prec, 2.0 / np.sqrt(k), 7, n, T)
+
+
+@pytest.mark.parametrize("prec", ["fp32", "bf16"])
+@pytest.mark.parametrize("k", [8, 16, 32, 64, 128])
+def test_score_every_rank_both_paths(X, prec, k):
+    for T in (5, 70):
+        note(f"score {prec} T={T} k={k}")
+        _check_score(X, _problem(k, T, 777, k, prec, None, 2), prec, 1.5 / np.sqrt(k), 64, 777, T)
+
+
+@pytest.mark.parametrize("scale", [0.0, -0.5, 30.0])
+def test_score_scales(X, scale):
+    """0: every score equal, ties to the lowest ids; a negative one; one that leaves almost all to one item."""
+    for prec in ("fp32", "bf16"):
+        for T in (3, 40):
+            note(f"score scale {scale} {prec} T={T}")
+            _check_score(X, _problem(5, T, 500, 16, prec, None, 2), prec, scale, 10, 500, T)
+
+
+@pytest.mark.parametrize("T", [2, 50])
+def test_score_all_excluded(X, T):
+    prob = _problem(3, T, 130, 32, "bf16", "all", 2)
+    r = _check_score(X, prob, "bf16", 1.0, 5, 130, T)
+    assert np.all(np.isneginf(r.lse.cpu().numpy())) and np.all(r.entropy.cpu().numpy() == 0)
+
+
+def test_best_items_of_equal_and_nearly_equal_rows(X):
+    """Copies of a few rows all over the table (ties go to the lowest id, across blocks and groups of blocks)."""
+    import torch
+    g = np.random.default_rng(8)
+    for T, n in ((2, 70000), (40, 70000)):
+        base = torch.from_numpy(g.standard_normal((50, 32)).astype(np.float32)).cuda()
+        F = base[torch.from_numpy(g.integers(0, 50, n)).cuda()]
+        H = torch.from_numpy(g.standard_normal((T, 32)).astype(np.float32)).cuda()
+        note(f"best items, equal rows T={T}")
+        r = X.score(H, F, top=64)
+        z = (H.double().cpu() @ base.double().cpu().t()).numpy()
+        best = z.argmax(1)
+        Fc, bc = F.cpu().numpy(), base.cpu().numpy()
+        for t in range(T):
+            same = np.flatnonzero((Fc == bc[best[t]]).all(1))[:64]
+            assert np.array_equal(r.top_ids[t].cpu().numpy(), same)
+
+
+def test_best_items_of_a_long_table(X):
+    """More blocks than groups of one block; best items at both ends and in the last, ragged block."""
+    import torch
+    n = 200_003
+    g = torch.Generator(device="cuda").manual_seed(4)
+    F = torch.randn((n, 16), generator=g, device="cuda").to(torch.bfloat16)
+    H = torch.randn((45, 16), generator=g, device="cuda").to(torch.bfloat16)
+    F[0] = F[-1] = F[100_000] = 4 * H[0]
+    note("best items of a long table")
+    for rows in (H, H[:1]):
+        r = X.score(rows, F, top=20, entropy=True)
+        z = rows.double() @ F.double().t()
+        order = torch.sort(z, dim=1, descending=True, stable=True)
+        assert torch.equal(r.top_ids.long(), order.indices[:, :20])
+        assert r.top_ids[0, :3].tolist() == [0, 100_000, n - 1]
+        lse = torch.logsumexp(z, 1)
+        zb = (2 * 16 + 16) * ref.U * (rows.double().abs() @ F.double().abs().t()).max(1).values
+        assert bool(((r.lse.double() - lse).abs() <= zb + (n / 16 + 72) * ref.U + 2 * ref.U * lse.abs()).all())
+
+
+@pytest.mark.parametrize("T,n,m,top", [(0, 10, 2, 3), (4, 0, 2, 3), (0, 0, 0, 0), (5, 3, 0, 10)])
+def test_empty_sizes(X, T, n, m, top):
+    import torch
+    H, F = torch.ones((T, 8), device="cuda"), torch.ones((n, 8), device="cuda")
+    ids = torch.full((T, m), -1, dtype=torch.int32, device="cuda") if m else None
+    r = X.score(H, F, ids=ids, top=top, entropy=True)
+    lse = r.lse.cpu().numpy()
+    assert lse.shape == (T,) and (n > 0 or np.all(np.isneginf(lse)))
+    assert np.all(r.entropy.cpu().numpy() == 0) if n == 0 else True
+    if top and T:
+        assert r.top_ids.cpu().numpy().tolist() == [[j if j < n else -1 for j in range(top)]] * T
+    dH, dF = X.score_grad(H, F, r.lse, ids=ids, dlogp=None if ids is None else torch.ones((T, m), device="cuda"))
+    assert dH.shape == H.shape and dF.shape == F.shape
+    assert torch.count_nonzero(dH) == 0 and torch.count_nonzero(dF) == 0
+    X.rows_check()
+
+
+def test_a_nan_row_stays_with_itself(X):
+    import torch
+    g = np.random.default_rng(1)
+    H, _ = _table(g, 40, 32, "bf16")
+    F, _ = _table(g, 300, 32, "bf16")
+    a = X.score(H, F, top=4, entropy=True)
+    H2 = H.clone()
+    H2[7, 3] = float("nan")
+    b = X.score(H2, F, top=4, entropy=True)
+    keep = torch.arange(40, device="cuda") != 7
+    for x, y in zip((a.lse, a.entropy, a.top_ids, a.top_logp), (b.lse, b.entropy, b.top_ids, b.top_logp)):
+        assert torch.equal(x[keep], y[keep])
+    assert bool(torch.isnan(b.lse[7]))
+
+
+# ---------------------------------------------------------------- gradients
+
+def _check_grads(got, dz, size, Hd, Fd, out, scale, tau, b, lse, prec):
+    T, n = dz.shape
+    s = float(np.float32(scale)) / tau
+    zb = ref.z_bound(Hd, Fd, out, scale, tau, b)
+    for x, w, bound, what in zip(got, ref.grads(dz, Hd, Fd, out, s),
+                                 ref.grad_bounds(size, Hd, Fd, out, s, zb, lse, n, T, prec == "bf16"), ("dH", "dF")):
+        _near(x, w, bound + (ref.V if prec == "bf16" else 2 * ref.U) * (np.abs(w) + bound), what)
+
+
+@pytest.mark.parametrize("prec", ["fp32", "bf16"])
+@pytest.mark.parametrize("bias", [None, "some"])
+@pytest.mark.parametrize("T,n", SIZES)
+def test_score_grad(X, prec, bias, T, n):
+    k = [8, 16, 32, 64, 128][(T + 2 * n) % 5]
+    g, H, Hd, F, Fd, b, ids = _problem(T + n, T, n, k, prec, bias, 4, ld=8 if n % 2 else 0)
+    out = np.zeros(n, bool) if b is None else b < ref.EXCLUDED
+    scale = 1.5 / np.sqrt(k)
+    gb = None if b is None else _gpu(b)
+    dlogp = g.standard_normal(ids.shape).astype(np.float32)
+    for dent in (None, g.standard_normal(T).astype(np.float32)):
+        note(f"score_grad {prec} T={T} n={n} k={k} bias={bias} entropy={dent is not None}")
+        r = X.score(H, F, ids=_gpu(ids, np.int32), scale=scale, bias=gb, entropy=True)
+        got = X.score_grad(H, F, r.lse, ids=_gpu(ids, np.int32), dlogp=_gpu(dlogp), scale=scale, bias=gb,
+                           **({} if dent is None else dict(entropy=r.entropy, dentropy=_gpu(dent))))
+        dz, size = ref.dz_score(Hd, Fd, ids, dlogp, dent, float(np.float32(scale)), b)
+        lse = ref.softmax_over(Hd, Fd, scale, b, 1.0)[1]
+        _check_grads(got, dz, size, Hd, Fd, out, scale, 1.0, b, lse, prec)
+        if dent is not None:  # one side at a time gives the same bits
+            import torch
+            half = [X.score_grad(H, F, r.lse, ids=_gpu(ids, np.int32), dlogp=_gpu(dlogp), entropy=r.entropy,
+                                 dentropy=_gpu(dent), scale=scale, bias=gb, want_H=q, want_F=not q)[0 if q else 1]
+                    for q in (True, False)]
+            assert torch.equal(half[0], got[0]) and torch.equal(half[1], got[1])
+    X.rows_check()
+
+
+@pytest.mark.parametrize("prec", ["fp32", "bf16"])
+@pytest.mark.parametrize("bias", [None, "some", "all"])
+@pytest.mark.parametrize("T,n,m,tau", [(1, 5, 1, 1.0), (3, 40, 8, 2.0), (33, 1000, 50, 4.0), (200, 160, 8, 1.0),
+                                       (300, 300, 20, 0.5), (70, 9, 70, 2.0)])
+def test_distill(X, prec, bias, T, n, m, tau):
+    k = [8, 16, 32, 64, 128][(T + m) % 5]
+    g, H, Hd, F, Fd, b, ids = _problem(T + m, T, n, k, prec, bias, m)
+    ids[0] = -1  # a row without a teacher
+    out = np.zeros(n, bool) if b is None else b < ref.EXCLUDED
+    scale = float(np.float32(1.5 / np.sqrt(k)))
+    teacher = (3 * g.standard_normal(ids.shape)).astype(np.float32)
+    teacher[-1, 0] = -np.inf if m > 1 else teacher[-1, 0]
+    dloss = g.standard_normal(T).astype(np.float32)
+    args = (H, F, _gpu(ids, np.int32), _gpu(teacher))
+    opts = dict(scale=scale, temperature=tau, bias=None if b is None else _gpu(b))
+    note(f"distill {prec} T={T} n={n} k={k} m={m} tau={tau} bias={bias}")
+    loss, lse = X.distill(*args, **opts)
+    want, wlse = ref.distill(Hd, Fd, ids, teacher, scale, b, tau)
+    zb = ref.z_bound(Hd, Fd, out, scale, tau, b)
+    lb = ref.lse_bound(zb, wlse, n)
+    _near(lse, wlse, lb, "lse")
+    _near(loss, want, tau * tau * lb + 4 * ref.U * np.abs(want), "loss")
+    got = X.distill_grad(*args, lse, _gpu(dloss), **opts)
+    dz, size = ref.dz_distill(Hd, Fd, ids, teacher, dloss, scale, b, tau)
+    _check_grads(got, dz, size, Hd, Fd, out, scale, tau, b, wlse, prec)
+    X.rows_check()
+
+
+@pytest.mark.parametrize("prec", ["fp32", "bf16"])
+def test_gradients_with_every_sum_split(X, prec):
+    """Long enough on both sides that the streamed side is cut into slices; and an item that every row lists."""
+    T, n, k, m = 1500, 5000, 64, 3
+    g, H, Hd, F, Fd, b, ids = _problem(12, T, n, k, prec, "some", m)
+    ids[:, 1] = int(np.flatnonzero(b > ref.EXCLUDED)[17])
+    out = b < ref.EXCLUDED
+    scale = float(np.float32(0.2))
+    dlogp, dent = g.standard_normal(ids.shape).astype(np.float32), g.standard_normal(T).astype(np.float32)
+    note(f"gradients, sliced {prec}")
+    r = X.score(H, F, ids=_gpu(ids, np.int32), scale=scale, bias=_gpu(b), entropy=True)
+    call = lambda: X.score_grad(H, F, r.lse, ids=_gpu(ids, np.int32), dlogp=_gpu(dlogp), entropy=r.entropy,  # noqa: E731
+                                dentropy=_gpu(dent), scale=scale, bias=_gpu(b))
+    got = call()
+    dz, size = ref.dz_score(Hd, Fd, ids, dlogp, dent, scale, b)
+    _check_grads(got, dz, size, Hd, Fd, out, scale, 1.0, b, ref.softmax_over(Hd, Fd, scale, b, 1.0)[1], prec)
+    import torch
+    again = call()
+    assert torch.equal(got[0], again[0]) and torch.equal(got[1], again[1])
+
+
+def test_gradient_against_differences_of_the_loss(X):
+    """A step of size e along a direction D: the loss's difference over 2 e is the gradient along D up to the
+    difference quotient's own error, which the definition in 64 bits has too."""
+    T, n, k, m, tau, e = 40, 300, 32, 6, 2.0, 2.0 ** -5
+    g, H, Hd, F, Fd, _, ids = _problem(21, T, n, k, "fp32", None, m)
+    teacher = (2 * g.standard_normal(ids.shape)).astype(np.float32)
+    scale = 0.25
+    ids_g, te_g = _gpu(ids, np.int32), _gpu(teacher)
+    loss = lambda A, B: X.distill(A, B, ids_g, te_g, scale=scale, temperature=tau)  # noqa: E731
+    l0, lse = loss(H, F)
+    import torch
+    dH, dF = X.distill_grad(H, F, ids_g, te_g, lse, torch.ones(T, device="cuda"), scale=scale, temperature=tau)
+    for side in range(2):
+        D = np.round(g.standard_normal(Hd.shape if side == 0 else Fd.shape) * 4) / 4
+        up, down = ((H + e * _gpu(D), F), (H - e * _gpu(D), F)) if side == 0 else ((H, F + e * _gpu(D)), (H, F - e * _gpu(D)))
+        quotient = (loss(*up)[0].double().sum() - loss(*down)[0].double().sum()).item() / (2 * e)
+        exact = sum(sgn * ref.distill(a.double().cpu().numpy(), f.double().cpu().numpy(), ids, teacher, scale, None, tau)[0].sum()
+                    for sgn, (a, f) in ((1, up), (-1, down))) / (2 * e)
+        along = float((((dH, dF)[side]).double().cpu().numpy() * D).sum())
+        dz, _ = ref.dz_distill(Hd, Fd, ids, teacher, np.ones(T), scale, None, tau)
+        true = float((ref.grads(dz, Hd, Fd, np.zeros(n, bool), scale / tau)[side] * D).sum())
+        lb = tau * tau * ref.lse_bound(ref.z_bound(Hd, Fd, np.zeros(n, bool), scale, tau, None) * 1.5, lse.cpu().numpy(), n)
+        noise = 2 * (lb.sum() + 4 * ref.U * float(l0.abs().sum())) / (2 * e)
+        assert abs(quotient - exact) <= noise, (quotient, exact, noise)
+        assert abs(along - quotient) <= noise + abs(true - exact) * 1.01 + 1e-4 * abs(true), (along, quotient)
+
+
+# ------------------------------------------------------------ used together
+
+def _training_step(X, P, F, users, ids, teacher, dloss, scale):
+    H = X.lookup(P, users, scale=2.0)
+    loss, lse = X.distill(H, F, ids, teacher, scale=scale, temperature=2.0)
+    dH, dF = X.distill_grad(H, F, ids, teacher, lse, dloss, scale=scale, temperature=2.0)
+    dP = X.lookup_grad(dH, users, P.shape[0], scale=2.0)
+    r = X.score(H, F, ids=ids, scale=scale, top=5, entropy=True)
+    return loss, lse, dH, dF, dP, r.lse, r.logp, r.entropy, r.top_ids, r.top_logp
+
+
+def _step_inputs(seed, prec="bf16"):
+    g = np.random.default_rng(seed)
+    P, _ = _table(g, 500, 64, prec)
+    F, _ = _table(g, 3001, 64, prec)
+    users = _gpu(g.integers(-1, 500, 300), np.int32)
+    ids = _gpu(g.integers(0, 3001, (300, 10)), np.int32)
+    return P, F, users, ids, _gpu(g.standard_normal((300, 10))), _gpu(g.random(300)), 0.2
+
+
+def test_a_training_step_and_its_answers(X):
+    """Lookup, distillation, both gradients and the lookup's: the gradient in P by the chain rule in 64 bits."""
+    P, F, users, ids, teacher, dloss, scale = _step_inputs(3, "fp32")
+    note("a training step")
+    loss, lse, dH, dF, dP, *_ = _training_step(X, P, F, users, ids, teacher, dloss, scale)
+    u, Pd, Fd = users.cpu().numpy(), P.double().cpu().numpy(), F.double().cpu().numpy()
+    Hd = np.where(u[:, None] >= 0, 2.0 * Pd[np.maximum(u, 0)], 0.0)
+    s = float(np.float32(scale))
+    dz, size = ref.dz_distill(Hd, Fd, ids.cpu().numpy(), teacher.cpu().numpy(), dloss.cpu().numpy(), s, None, 2.0)
+    none = np.zeros(F.shape[0], bool)
+    wH, wF = ref.grads(dz, Hd, Fd, none, s / 2)
+    zb = ref.z_bound(Hd, Fd, none, s, 2.0, None)
+    bH, bF = ref.grad_bounds(size, Hd, Fd, none, s / 2, zb, lse.cpu().numpy(), F.shape[0], 300, False)
+    _near(dH, wH, bH + 2 * ref.U * np.abs(wH), "dH")
+    _near(dF, wF, bF + 2 * ref.U * np.abs(wF), "dF")
+    want, bound = np.zeros(P.shape), np.zeros(P.shape)
+    np.add.at(want, u[u >= 0], 2 * wH[u >= 0])
+    np.add.at(bound, u[u >= 0], 2 * (bH + 66 * ref.U * np.abs(wH))[u >= 0])
+    _near(dP, want, bound * 1.01, "dP")
+    X.rows_check()
+
+
+def test_captured_steps_replay_the_eager_results(X):
+    """Two graphs of the step on one handle, replayed with new inputs, in turn and with eager work between."""
+    import torch
+    note("captured steps")
+    sets = [_step_inputs(s) for s in (5, 6)]
+    side = torch.cuda.Stream()
+    graphs = []
+    with torch.cuda.stream(side):
+        for st in sets:
+            _training_step(X, *st)
+    side.synchronize()
+    for st in sets:
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=side):
+            out = _training_step(X, *st)
+        graphs.append((g, out))
+    for turn in range(4):
+        new = [_step_inputs(50 + 2 * turn + q) for q in range(2)]
+        for st, fresh in zip(sets, new):
+            for a, b in zip(st[:-1], fresh[:-1]):
+                a.copy_(b)
+        for g, _ in graphs:
+            g.replay()
+        eager = [_training_step(X, *st) for st in sets]
+        torch.cuda.synchronize()
+        for (_, out), want in zip(graphs, eager):
+            for a, b in zip(out, want):
+                assert torch.equal(a, b)
+    X.rows_check()
+
+
+def test_calls_on_two_streams_at_once(X):
+    """They share nothing: the same bits as one after the other."""
+    import torch
+    sets = [_step_inputs(s) for s in (7, 8)]
+    alone = [_training_step(X, *st) for st in sets]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in sets]
+    for _ in range(3):
+        outs = []
+        for st, s in zip(sets, streams):
+            with torch.cuda.stream(s):
+                outs.append(_training_step(X, *st))
+        torch.cuda.synchronize()
+        for a, b in zip(outs, alone):
+            for x, y in zip(a, b):
+                assert torch.equal(x, y)
+
+
+def test_a_capture_is_not_checked(X):
+    import torch
+    import paper_2608_00977_amd as tsid
+    F, ids = torch.ones((10, 8), device="cuda"), _gpu([1], np.int32)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        out = X.lookup(F, ids)
+        with pytest.raises(tsid.TsidError) as e:
+            X.rows_check()
+    assert e.value.status == 6
+    g.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(out, F[:1])
+
+
+# ----------------------------------------------------------------- refusals
+
+def _refused(status, f, *a, **kw):
+    import paper_2608_00977_amd as tsid
+    with pytest.raises(tsid.TsidError) as e:
+        f(*a, **kw)
+    assert e.value.status == status, str(e.value)
+
+
+def test_refusals(X):
+    """Each is refused on the host, before any launch, and leaves the outputs as they were."""
+    import torch
+    z = lambda *s, dt=torch.float32: torch.zeros(s, dtype=dt, device="cuda")  # noqa: E731
+    i = lambda *s: torch.zeros(s, dtype=torch.int32, device="cuda")  # noqa: E731
+    H, F = z(4, 16), z(9, 16)
+    note("refusals")
+    for bad in (z(4, 12), z(4, 24), z(4, 256), z(4, 16, dt=torch.float16), z(4, 16, 1), z(16, 9).t()[:, :8],
+                z(4, 16).cpu(), z(5 * 18)[:72].view(4, 18)[:, :16], z(81)[1:65].view(4, 16)):
+        _refused(1, X.lookup, bad, i(2))
+        _refused(1, X.score, bad, F if bad.dim() != 2 or bad.shape[1] == 16 else z(9, bad.shape[1]))
+        _refused(1, X.lookup_grad, bad, i(bad.shape[0]), 3)
+    _refused(1, X.lookup, F, i(2).long())
+    _refused(1, X.lookup, F, i(2), out=z(3, 16))
+    _refused(1, X.lookup, F, i(2), out=z(2, 16, dt=torch.bfloat16))
+    _refused(1, X.lookup_grad, H, i(3), 5)
+    _refused(1, X.lookup_grad, H, i(4), 5, out=z(6, 16))
+    _refused(1, X.score, H, z(9, 32))
+    _refused(1, X.score, H, F.bfloat16())
+    _refused(1, X.score, H, F, bias=z(8))
+    _refused(1, X.score, H, F, ids=i(3, 2))
+    _refused(1, X.score, H, F, ids=i(4, 2).long())
+    _refused(1, X.score, H, F, top=65)
+    _refused(1, X.score, H, F, top=-1)
+    for s in (float("nan"), float("inf"), 1e39):
+        _refused(1, X.score, H, F, scale=s)
+    te, lse = z(4, 2), z(4)
+    for tau in (0.0, -1.0, 1e-7, 1e7, float("nan")):
+        _refused(1, X.distill, H, F, i(4, 2), te, temperature=tau)
+        _refused(1, X.distill_grad, H, F, i(4, 2), te, lse, lse, temperature=tau)
+    _refused(1, X.distill, H, F, i(4, 2), z(4, 3))
+    _refused(1, X.distill, H, F, i(4, 0), z(4, 0))
+    _refused(1, X.score_grad, H, F, z(3))
+    _refused(1, X.score_grad, H, F, lse, dlogp=te)
+    _refused(1, X.score_grad, H, F, lse, entropy=lse)
+    _refused(1, X.score_grad, H, F, lse, dentropy=lse)
+    X.rows_check()
+
+
+def test_refusals_of_the_library(X):
+    """The C entry points' own checks: workspaces, outputs' shapes, NULL pointers."""
+    import ctypes as C
+    import torch
+    from paper_2608_00977_amd import binding as B
+    H, F = torch.ones((4, 16), device="cuda"), torch.ones((9, 16), device="cuda")
+    rows = lambda x: B.tsid_rows(x.data_ptr(), x.shape[0], x.stride(0))  # noqa: E731
+    lse = torch.full((4,), 5.0, device="cuda")
+    need = B.tsid_score_workspace(4, 9, 16, 0)
+    ws = torch.zeros(need + 512, dtype=torch.uint8, device="cuda")
+    at = (ws.data_ptr() + 255) & ~255
+    head = B.tsid_head(rows(H), rows(F), None, 16, 0, 1.0, 1.0)
+    call = lambda hd=head, w=at, n=need, ids=None, m=0, top=0, out=lse.data_ptr(): B.tsid_score(  # noqa: E731
+        X.ctx, hd, ids, m, top, out, None, None, None, None, w, n)
+    assert call(w=None) == 1 and call(w=at + 16) == 1 and call(n=need - 1) == 1
+    assert call(m=-1) == 1 and call(m=1) == 1 and call(top=1) == 1 and call(top=65) == 1 and call(out=lse.data_ptr() + 2) == 1
+    for field, value in (("k", 24), ("prec", 2), ("scale", float("nan")), ("temperature", 0.0)):
+        hd = B.tsid_head(rows(H), rows(F), None, 16, 0, 1.0, 1.0)
+        setattr(hd, field, value)
+        assert call(hd=hd) == 1, field
+    for r in (B.tsid_rows(H.data_ptr(), -1, 16), B.tsid_rows(H.data_ptr(), 2 ** 31, 16), B.tsid_rows(None, 4, 16),
+              B.tsid_rows(H.data_ptr(), 4, 15), B.tsid_rows(H.data_ptr(), 4, 18), B.tsid_rows(H.data_ptr() + 8, 3, 16)):
+        assert call(hd=B.tsid_head(r, rows(F), None, 16, 0, 1.0, 1.0)) == 1
+    assert B.lib().tsid_score(X.ctx, None, None, 0, 0, None, None, None, None, None, at, need, None) == 1
+    assert lse.cpu().tolist() == [5.0] * 4
+    need = B.tsid_head_grad_workspace(4, 9, 16, 0, 0)
+    ws = torch.zeros(need + 512, dtype=torch.uint8, device="cuda")
+    at = (ws.data_ptr() + 255) & ~255
+    grad = lambda dH, dF: B.tsid_score_grad(X.ctx, head, None, 0, lse.data_ptr(), None, None, None, dH, dF, at, need)  # noqa: E731
+    assert grad(rows(F), None) == 1 and grad(None, rows(H)) == 1 and grad(None, None) == 0
+    torch.cuda.synchronize()
+    assert B.lib().tsid_lookup(X.ctx, 0, 16, None, None, C.c_float(1.0), None, None) == 1
