@@ -584,7 +584,7 @@ typedef struct {
  *  top      0 .. TSID_MAX_TOP: the items of the largest z, largest first, ties
  *           to the lowest id; top_ids and top_logp are T x top (-1 and -inf
  *           beyond the items that are not excluded).  Candidates are found with
- *           scores in fp32 (blocks of 32 items by their largest score, 16 blocks
+ *           scores in fp32 (blocks of 32 items by their largest score, 8 blocks
  *           more than needed) and ranked by scores in fp64. */
 #define TSID_MAX_TOP 64
 size_t tsid_score_workspace(int64_t T, int64_t n, int32_t k, int32_t prec, int32_t top);

@@ -26,6 +26,15 @@ namespace tsid {
 
 namespace {
 
+#ifndef TSID_SCORE_CX
+#define TSID_SCORE_CX 2
+#endif
+#ifndef TSID_SCORE_WAVES
+#define TSID_SCORE_WAVES 2
+#endif
+#ifndef TSID_SCORE_GRID
+#define TSID_SCORE_GRID 4
+#endif
 constexpr int kThreads = 256;
 constexpr double kLog2e = 1.4426950408889634074, kLn2 = 0.69314718055994530942;
 constexpr float kOff = -2e30f;    // the exponent's offset at an excluded item
@@ -286,7 +295,7 @@ inline int grid_of(int32_t n_slices, int32_t n_tiles) {
 // Many rows: four waves of CX * 32 rows each share tiles of F through LDS, two
 // tiles deep (one is read while the next one's loads are in flight).
 template <int K, int NP, int CX, int YT, bool ENT>
-__global__ __launch_bounds__(kThreads, 2) void k_score_pass(ScoreK A) {
+__global__ __launch_bounds__(kThreads, TSID_SCORE_WAVES) void k_score_pass(ScoreK A) {
     using TL = Tile<K, NP, YT>;
     extern __shared__ __align__(16) unsigned char smem[];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, h = lane >> 5;
@@ -421,24 +430,32 @@ __global__ __launch_bounds__(kThreads, 2) void k_score_few(ScoreK A) {
     }
 }
 
-// sup[g][t] = the largest of blkmax[b][t] over the G blocks of group g.
+// sup[t][g] = the largest of blkmax[b][t] over the G blocks of group g: tiles
+// of 32 rows and 32 groups, turned through LDS, so that both sides move lines.
 __global__ __launch_bounds__(kThreads) void k_block_groups(const float *blkmax, int64_t T, int64_t nblk, int64_t G,
-                                                           int64_t ngrp, float *sup) {
-    const int64_t j = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-    if (j >= ngrp * T) return;
-    const int64_t g = j / T, t = j % T;
-    const int64_t b1 = std::min<int64_t>((g + 1) * G, nblk);
-    float v = kOff;
-    for (int64_t b = g * G; b < b1; ++b) v = fmaxf(v, blkmax[b * T + t]);
-    sup[j] = v;
+                                                           int64_t ngrp, int64_t row_tiles, float *sup) {
+    __shared__ float turn[32][33];
+    const int x = threadIdx.x & 31, y = threadIdx.x >> 5;
+    const int64_t t0 = blockIdx.x % row_tiles * 32, g0 = blockIdx.x / row_tiles * 32;
+    for (int q = y; q < 32; q += kThreads / 32) {
+        const int64_t b0 = (g0 + q) * G, b1 = std::min<int64_t>(b0 + G, nblk);
+        float v = kOff;
+        if (t0 + x < T)
+            for (int64_t b = b0; b < b1; ++b) v = fmaxf(v, blkmax[b * T + t0 + x]);
+        turn[q][x] = v;
+    }
+    __syncthreads();
+    for (int q = y; q < 32; q += kThreads / 32)
+        if (t0 + q < T && g0 + x < ngrp) sup[(t0 + q) * ngrp + g0 + x] = turn[x][q];
 }
 
 // ------------------------------------------------- a row's results
 
-constexpr int kMargin = 16;                     // blocks beyond the wanted best items that are looked at
+constexpr int kMargin = 8;        // blocks beyond the wanted best items that are looked at
 constexpr int kMaxPick = TSID_MAX_TOP + kMargin;
-constexpr int kSelCap = 4096;                   // candidates chosen from at a time
-constexpr int kMaxGroups = 2048;
+constexpr int kSelCap = 2048;     // candidates chosen from at a time
+constexpr int kMaxGroups = 2048;  // one round of them
+constexpr int kCandBytes = kMaxPick * 32 * 8 > kSelCap * 8 ? kMaxPick * 32 * 8 : kSelCap * 8;
 
 // Larger floats have larger keys; NaN is below everything.
 __device__ __forceinline__ uint32_t order_key(float v) {
@@ -454,7 +471,8 @@ __device__ __forceinline__ uint64_t order_key(double v) {
 
 struct SelectLds {
     uint32_t hist[256], wsum[4];
-    uint32_t digit, need, count;
+    uint32_t digit, need, count, found;
+    int32_t place[kThreads];
 };
 
 // Sum over the threads before this one of the 256, and all of them.
@@ -478,64 +496,87 @@ __device__ __forceinline__ uint32_t before(uint32_t v, uint32_t *wsum, uint32_t 
     return pre + incl - v;
 }
 
-// Places (ascending) of the `want` largest of key[0 .. N - 1] to place[0 ..];
-// equal keys: the first ones.  Digit by digit from the top, until the keys
-// that share the digits so far are all wanted.  Returns how many.
+// The `want` (at most kMaxPick) largest of key[0 .. N - 1], equal keys in
+// order of place: returns in thread j < min(want, N) the place of the j-th, and
+// -1 elsewhere.  The keys' digits are gone through from the top until no more
+// than 256 keys can still be among them, which are then ranked by counting;
+// only where more are equal to the last bit are the first of them taken.
 template <typename U>
-__device__ int select_largest(const U *key, int N, int want, int32_t *place, SelectLds &L) {
+__device__ int32_t select_largest(const U *key, int N, int want, SelectLds &L) {
     const int t = threadIdx.x;
-    if (want >= N) {
-        for (int j = t; j < N; j += kThreads) place[j] = j;
+    if (want > N) want = N;
+    int have = N;
+    if (N <= kThreads) {
+        if (t < N) L.place[t] = t;
         __syncthreads();
-        return N;
-    }
-    U prefix = 0, mask = 0;
-    uint32_t need = (uint32_t)want;
-    bool all = false;
-    for (int shift = (int)sizeof(U) * 8 - 8; shift >= 0 && !all; shift -= 8) {
-        L.hist[t] = 0u;
-        __syncthreads();
-        for (int j = t; j < N; j += kThreads)
-            if ((key[j] & mask) == prefix) atomicAdd(&L.hist[(uint32_t)(key[j] >> shift) & 255u], 1u);
-        __syncthreads();
-        uint32_t total;
-        const uint32_t mine = L.hist[255 - t];  // thread t: digit 255 - t
-        const uint32_t above = before(mine, L.wsum, total);
-        if (above < need && need <= above + mine) {
-            L.digit = 255u - t;
-            L.need = need - above;
-            L.count = mine;
+    } else {
+        U prefix = 0, mask = 0;
+        uint32_t need = (uint32_t)want, left = (uint32_t)N;
+        for (int shift = (int)sizeof(U) * 8 - 8; shift >= 0 && left > (uint32_t)kThreads; shift -= 8) {
+            L.hist[t] = 0u;
+            __syncthreads();
+            for (int j = t; j < N; j += kThreads)
+                if ((key[j] & mask) == prefix) atomicAdd(&L.hist[(uint32_t)(key[j] >> shift) & 255u], 1u);
+            __syncthreads();
+            uint32_t total;
+            const uint32_t mine = L.hist[255 - t];  // thread t: digit 255 - t
+            const uint32_t above = before(mine, L.wsum, total);
+            if (above < need && need <= above + mine) {
+                L.digit = 255u - t;
+                L.need = need - above;
+                L.count = mine;
+            }
+            __syncthreads();
+            prefix |= (U)L.digit << shift;
+            mask |= (U)255u << shift;
+            need = L.need;
+            left = (uint32_t)want - need + L.count;
+            __syncthreads();
+        }
+        if (left <= (uint32_t)kThreads) {
+            if (t == 0) L.found = 0u;
+            __syncthreads();
+            for (int j = t; j < N; j += kThreads)
+                if ((key[j] & mask) >= prefix) L.place[atomicAdd(&L.found, 1u)] = j;
+            have = (int)left;
+        } else {  // the first `need` of the keys equal to prefix
+            const int per = (N + kThreads - 1) / kThreads, j0 = t * per, j1 = j0 + per < N ? j0 + per : N;
+            uint32_t eq = 0, take = 0, total;
+            for (int j = j0; j < j1; ++j) eq += key[j] == prefix;
+            const uint32_t eq_before = before(eq, L.wsum, total);
+            uint32_t e = eq_before;
+            for (int j = j0; j < j1; ++j) take += key[j] > prefix || (key[j] == prefix && e++ < need);
+            uint32_t at = before(take, L.wsum, total);
+            e = eq_before;
+            for (int j = j0; j < j1; ++j)
+                if (key[j] > prefix || (key[j] == prefix && e++ < need)) L.place[at++] = j;
+            have = want;
         }
         __syncthreads();
-        prefix |= (U)L.digit << shift;
-        mask |= (U)255u << shift;
-        need = L.need;
-        all = L.count == need;
-        __syncthreads();
     }
-    const int per = (N + kThreads - 1) / kThreads, j0 = t * per, j1 = j0 + per < N ? j0 + per : N;
-    uint32_t eq = 0, total;
-    for (int j = j0; j < j1; ++j) eq += (key[j] & mask) == prefix;
-    uint32_t eq_before = before(eq, L.wsum, total), take = 0, e = eq_before;
-    for (int j = j0; j < j1; ++j) {
-        const U v = key[j] & mask;
-        take += v > prefix || (v == prefix && e++ < need);
-    }
-    uint32_t at = before(take, L.wsum, total);
-    e = eq_before;
-    for (int j = j0; j < j1; ++j) {
-        const U v = key[j] & mask;
-        if (v > prefix || (v == prefix && e++ < need)) place[at++] = j;
+    int rank = kThreads;
+    int32_t mine = 0;
+    if (t < have) {
+        mine = L.place[t];
+        const U k = key[mine];
+        rank = 0;
+        for (int j = 0; j < have; ++j) {
+            const int32_t p = L.place[j];
+            rank += key[p] > k || (key[p] == k && p < mine);
+        }
     }
     __syncthreads();
-    return (int)total;
+    if (rank < want) L.place[rank] = mine;
+    __syncthreads();
+    const int32_t out = t < want ? L.place[t] : -1;
+    __syncthreads();
+    return out;
 }
 
 struct FinishK {
     const float4 *part;
     int32_t n_parts;
     Side H, F;
-    int32_t k;
     double scale, bias_scale;
     int64_t t0, T;
     const int32_t *ids;
@@ -552,12 +593,14 @@ struct FinishK {
     int32_t *err;
 };
 
-template <typename E>
-__device__ __forceinline__ double value(const E *p);
-template <>
-__device__ __forceinline__ double value(const float *p) { return (double)*p; }
-template <>
-__device__ __forceinline__ double value(const uint16_t *p) { return (double)__uint_as_float((uint32_t)*p << 16); }
+// Eight factors.
+__device__ __forceinline__ f8 load8(const float *p) {
+    const f4 a = *reinterpret_cast<const f4 *>(p), b = *reinterpret_cast<const f4 *>(p + 4);
+    return f8{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+}
+__device__ __forceinline__ f8 load8(const uint16_t *p) {
+    return __builtin_convertvector(__builtin_bit_cast(b8, *reinterpret_cast<const uint4 *>(p)), f8);
+}
 
 __device__ __forceinline__ double block_sum(double v, double *red) {
 #pragma unroll
@@ -577,21 +620,19 @@ __device__ __forceinline__ float block_max(float v, double *red) {
 }
 
 // One workgroup per row: the slices' sums joined in fp64, the given items'
-// scores in fp64, and the best items.  The best `top` items lie in the `top`
-// blocks of 32 whose maxima are largest (an item outside them has `top` better
-// ones), so those blocks and kMargin more, for the rounding of the maxima, are
-// scored again in fp64 and the best are ranked by these scores.  The blocks are
-// found through groups of blocks in the same way.
-template <typename E>
+// scores in fp64 (k / 8 lanes each), and the best items.  The best `top` items
+// lie in the `top` blocks of 32 whose maxima are largest (an item outside them
+// has `top` better ones), so those blocks and kMargin more, for the rounding of
+// the maxima, are scored again in fp64 and ranked by these scores.  The blocks
+// are found through groups of blocks in the same way.
+template <typename E, int K, bool TOP>
 __global__ __launch_bounds__(kThreads) void k_score_finish(FinishK A) {
-    __shared__ double hrow[128], red[4];
-    __shared__ __align__(16) unsigned char cand[kSelCap * 8];
-    __shared__ int32_t pick[2][kMaxPick], place_[kMaxPick];
-    __shared__ SelectLds L;
-    const int tid = threadIdx.x;
+    constexpr int LN = K / 8, NI = kThreads / LN;  // lanes of an item, items at a time
+    __shared__ double red[4];
+    const int tid = threadIdx.x, sub = tid % LN;
     const int64_t row = blockIdx.x, t = A.t0 + row;
-    const E *H = static_cast<const E *>(A.H.p), *F = static_cast<const E *>(A.F.p);
-    if (tid < A.k) hrow[tid] = value(H + t * A.H.ld + tid);
+    const E *F = static_cast<const E *>(A.F.p);
+    const f8 hv = load8(static_cast<const E *>(A.H.p) + t * A.H.ld + sub * 8);
     // log sum and entropy
     float m = kLeast;
     for (int q = tid; q < A.n_parts; q += kThreads) m = fmaxf(m, A.part[(int64_t)q * A.T + row].x);
@@ -612,22 +653,22 @@ __global__ __launch_bounds__(kThreads) void k_score_finish(FinishK A) {
         if (A.lse) A.lse[t] = (float)lse;
         if (A.entropy) A.entropy[t] = empty ? 0.f : (float)(kLn2 * (log2(s) - e / s));
     }
-    // the given items: 16 lanes each
-    const int sub = tid & 15;
-    auto usable = [&](int32_t id) { return id >= 0 && id < A.F.count && !(A.F.bias && A.F.bias[id] < kExcluded); };
-    auto logp_of = [&](int32_t id) {
+    auto usable = [&](int64_t id) { return id >= 0 && id < A.F.count && !(A.F.bias && A.F.bias[id] < kExcluded); };
+    // the score of an item whose factors f the LN lanes hold
+    auto score_of = [&](int64_t id, const f8 &f) {
         double z = 0.0;
-        for (int c = sub; c < A.k; c += 16) z = fma(hrow[c], value(F + (int64_t)id * A.F.ld + c), z);
 #pragma unroll
-        for (int off = 8; off > 0; off >>= 1) z += __shfl_xor(z, off, 16);
-        return z * A.scale + (A.F.bias ? (double)A.F.bias[id] * A.bias_scale : 0.0) - lse;
+        for (int c = 0; c < 8; ++c) z = fma((double)hv[c], (double)f[c], z);
+#pragma unroll
+        for (int off = LN / 2; off > 0; off >>= 1) z += __shfl_xor(z, off, LN);
+        return z * A.scale + (A.F.bias ? (double)A.F.bias[id] * A.bias_scale : 0.0);
     };
     const int32_t *ids = A.ids ? A.ids + t * A.per_row : nullptr;
     if (A.logp) {
-        for (int j = tid >> 4; j < A.per_row; j += kThreads / 16) {
+        for (int j = tid / LN; j < A.per_row; j += NI) {
             const int32_t id = ids[j];
             float v = 0.f;
-            if (usable(id)) v = (float)logp_of(id);
+            if (usable(id)) v = (float)(score_of(id, load8(F + (int64_t)id * A.F.ld + sub * 8)) - lse);
             else if (id >= 0 && id < A.F.count) v = -INFINITY;
             else if (id != -1) A.err[ERR_RANGE] = 1;
             if (sub == 0) A.logp[t * A.per_row + j] = v;
@@ -644,13 +685,14 @@ __global__ __launch_bounds__(kThreads) void k_score_finish(FinishK A) {
         tm = block_max(tm, red);
         double w_sum = 0.0, a_sum = 0.0;
         if (tm > -INFINITY) {
-            for (int j = tid >> 4; j < A.per_row; j += kThreads / 16) {
-                if (!usable(ids[j])) continue;
+            for (int j = tid / LN; j < A.per_row; j += NI) {
+                const int32_t id = ids[j];
+                if (!usable(id)) continue;
                 const double lw = ((double)tl[j] - (double)tm) / A.tau, w = exp(lw);
-                const double lp = logp_of(ids[j]);
+                const double z = score_of(id, load8(F + (int64_t)id * A.F.ld + sub * 8));
                 if (sub == 0 && w > 0.0) {
                     w_sum += w;
-                    a_sum += w * (lw - lp);
+                    a_sum += w * (lw - (z - lse));
                 }
             }
         }
@@ -658,100 +700,117 @@ __global__ __launch_bounds__(kThreads) void k_score_finish(FinishK A) {
         a_sum = block_sum(a_sum, red);
         if (tid == 0) A.loss[t] = w_sum > 0.0 ? (float)(A.tau * A.tau * (a_sum / w_sum - log(w_sum))) : 0.f;
     }
-    if (A.top <= 0) return;
-    // the blocks that hold the best items
-    uint32_t *key = reinterpret_cast<uint32_t *>(cand);
-    int32_t *pay = reinterpret_cast<int32_t *>(cand + kSelCap * 4);
-    // the `want` largest of total candidates get(j) -> (value, payload), payloads ascending, to out
-    auto choose = [&](int64_t total, int want, int32_t *out, auto get) {
-        int have = 0;
-        int64_t next = 0;
-        do {
-            const int n_new = (int)std::min<int64_t>(kSelCap - have, total - next);
-            for (int j = tid; j < n_new; j += kThreads) {
-                float v;
-                int32_t p;
-                get(next + j, v, p);
-                key[have + j] = order_key(v);
-                pay[have + j] = p;
-            }
-            __syncthreads();
-            const int got = select_largest(key, have + n_new, want, place_, L);
-            next += n_new;
-            if (next < total) {  // keep them at the front for the next round
-                uint32_t k0 = 0;
-                int32_t p0 = 0;
-                if (tid < got) {
-                    k0 = key[place_[tid]];
-                    p0 = pay[place_[tid]];
+    if constexpr (TOP) {
+        __shared__ __align__(16) unsigned char cand[kCandBytes];
+        __shared__ int32_t pick[2][kMaxPick];
+        __shared__ SelectLds L;
+        uint32_t *key = reinterpret_cast<uint32_t *>(cand);
+        int32_t *pay = reinterpret_cast<int32_t *>(cand + kSelCap * 4);
+        // the `want` largest of `total` candidates get(j, value, payload), best first, to out
+        auto choose = [&](int64_t total, int want, int32_t *out, auto get) {
+            int have = 0;
+            int64_t next = 0;
+            do {
+                const int n_new = (int)std::min<int64_t>(kSelCap - have, total - next);
+                for (int j = tid; j < n_new; j += kThreads) {
+                    float v;
+                    int32_t p;
+                    get(next + j, v, p);
+                    key[have + j] = order_key(v);
+                    pay[have + j] = p;
                 }
                 __syncthreads();
-                if (tid < got) {
+                next += n_new;
+                const int32_t place = select_largest(key, have + n_new, want, L);
+                have = std::min(have + n_new, want);
+                uint32_t k0 = 0;
+                int32_t p0 = 0;
+                if (place >= 0) {
+                    k0 = key[place];
+                    p0 = pay[place];
+                }
+                __syncthreads();
+                if (place >= 0) {  // the front of the next round
                     key[tid] = k0;
                     pay[tid] = p0;
+                    out[tid] = p0;
                 }
-            } else {
-                if (tid < got) out[tid] = pay[place_[tid]];
+                __syncthreads();
+            } while (next < total);
+            return have;
+        };
+        const int want = A.top + kMargin;
+        int got;
+        if (A.sup) {
+            const float *sup = A.sup + row * A.ngrp;
+            const int groups = choose(A.ngrp, want, pick[0], [&](int64_t j, float &v, int32_t &p) {
+                v = sup[j];
+                p = (int32_t)j;
+            });
+            // in ascending order of blocks, for the ties
+            int32_t g = 0;
+            int rank = 0;
+            if (tid < groups) {
+                g = pick[0][tid];
+                for (int j = 0; j < groups; ++j) rank += pick[0][j] < g;
             }
-            have = got;
             __syncthreads();
-        } while (next < total);
-        return have;
-    };
-    const int want = A.top + kMargin;
-    int got;
-    if (A.sup) {
-        const int groups = choose(A.ngrp, want, pick[0], [&](int64_t j, float &v, int32_t &p) {
-            v = A.sup[j * A.T + row];
-            p = (int32_t)j;
-        });
-        got = choose(groups * A.G, want, pick[1], [&](int64_t j, float &v, int32_t &p) {
-            const int64_t b = pick[0][j / A.G] * A.G + j % A.G;
-            v = b < A.nblk ? A.blkmax[b * A.T + row] : -INFINITY;
-            p = (int32_t)b;
-        });
-    } else {
-        got = choose(A.nblk, want, pick[1], [&](int64_t j, float &v, int32_t &p) {
-            v = A.blkmax[j * A.T + row];
-            p = (int32_t)j;
-        });
-    }
-    // their items in fp64, one lane per item
-    uint64_t *key64 = reinterpret_cast<uint64_t *>(cand);
-    for (int j = tid; j < got * 32; j += kThreads) {
-        const int64_t id = (int64_t)pick[1][j >> 5] * 32 + (j & 31);
-        uint64_t kv = 0ull;
-        if (id < A.F.count && usable((int32_t)id)) {
-            double z = 0.0;
-            const E *f = F + id * A.F.ld;
-#pragma unroll 8
-            for (int c = 0; c < A.k; ++c) z = fma(hrow[c], value(f + c), z);
-            z = z * A.scale + (A.F.bias ? (double)A.F.bias[id] * A.bias_scale : 0.0);
-            kv = order_key(z);
+            if (tid < groups) pick[0][rank] = g;
+            __syncthreads();
+            got = choose(groups * A.G, want, pick[1], [&](int64_t j, float &v, int32_t &p) {
+                const int64_t b = pick[0][j / A.G] * A.G + j % A.G;
+                v = b < A.nblk ? A.blkmax[b * A.T + row] : -INFINITY;
+                p = (int32_t)b;
+            });
+        } else {
+            got = choose(A.nblk, want, pick[1], [&](int64_t j, float &v, int32_t &p) {
+                v = A.blkmax[j * A.T + row];
+                p = (int32_t)j;
+            });
         }
-        key64[j] = kv;
-    }
-    __syncthreads();
-    const int best = select_largest(key64, got * 32, A.top, place_, L);
-    if (tid < A.top) {
-        int32_t id = -1;
-        float lp = -INFINITY;
-        int rank = tid;
-        if (tid < best) {
-            const uint64_t kv = key64[place_[tid]];
-            rank = 0;
-            for (int j = 0; j < best; ++j) {
-                const uint64_t o = key64[place_[j]];
-                rank += o > kv || (o == kv && j < tid);
+        // their items, best first
+        int32_t b0 = 0;
+        int rank = 0;
+        if (tid < got) {
+            b0 = pick[1][tid];
+            for (int j = 0; j < got; ++j) rank += pick[1][j] < b0;
+        }
+        __syncthreads();
+        if (tid < got) pick[0][rank] = b0;  // ascending, for the ties
+        __syncthreads();
+        uint64_t *key64 = reinterpret_cast<uint64_t *>(cand);
+        constexpr int U = 4;  // items of a lane group in flight
+        for (int j0 = tid / LN; j0 < got * 32; j0 += NI * U) {
+            f8 f[U];
+            int64_t id[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int j = j0 + u * NI;
+                id[u] = j < got * 32 ? (int64_t)pick[0][j >> 5] * 32 + (j & 31) : -1;
+                if (!usable(id[u])) id[u] = -1;
+                f[u] = load8(F + std::max<int64_t>(id[u], 0) * A.F.ld + sub * 8);
             }
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int j = j0 + u * NI;
+                const double z = score_of(std::max<int64_t>(id[u], 0), f[u]);
+                if (sub == 0 && j < got * 32) key64[j] = id[u] >= 0 ? order_key(z) : 0ull;
+            }
+        }
+        __syncthreads();
+        const int32_t place = select_largest(key64, got * 32, A.top, L);
+        if (tid < A.top) {
+            int32_t id = -1;
+            float lp = -INFINITY;
+            const uint64_t kv = place >= 0 ? key64[place] : 0ull;
             if (kv != 0ull) {
-                id = pick[1][place_[tid] >> 5] * 32 + (place_[tid] & 31);
+                id = pick[0][place >> 5] * 32 + (place & 31);
                 const double z = __longlong_as_double((long long)((kv >> 63) ? kv & ~(1ull << 63) : ~kv));
                 lp = (float)(z - lse);
             }
+            A.top_ids[t * A.top + tid] = id;
+            A.top_logp[t * A.top + tid] = lp;
         }
-        A.top_ids[t * A.top + rank] = id;
-        A.top_logp[t * A.top + rank] = lp;
     }
 }
 
@@ -961,6 +1020,9 @@ __global__ __launch_bounds__(kThreads, 2) void k_grad_pass(GradK A) {
     }
 }
 
+__device__ __forceinline__ float factor(float v) { return v; }
+__device__ __forceinline__ float factor(uint16_t v) { return __uint_as_float((uint32_t)v << 16); }
+
 // out[t] = scale (a_t * sum of the parts + sum_j w_tj F[id_tj]) (a_t in the parts already: coef null).
 template <typename E>
 __global__ __launch_bounds__(kThreads) void k_grad_rows(const float *part, int32_t n_parts, int64_t T, int k,
@@ -980,7 +1042,7 @@ __global__ __launch_bounds__(kThreads) void k_grad_rows(const float *part, int32
         if (v == 0.f) continue;  // also the entries that are no item's
         const E *f = F + (int64_t)ids[t * per_row + q] * ldf + c;
 #pragma unroll
-        for (int x = 0; x < 4; ++x) more[x] = fmaf(v, (float)value(f + x), more[x]);
+        for (int x = 0; x < 4; ++x) more[x] = fmaf(v, factor(f[x]), more[x]);
     }
     sum = (sum + more) * scale;
     if constexpr (sizeof(E) == 4) {
@@ -1026,14 +1088,14 @@ ScorePlan plan_score(int64_t T, int64_t n, int prec, int top, Carve &c) {
         const int64_t most = std::max<int64_t>(256, (int64_t(1) << 28) / std::max<int64_t>(p.nblk, 1) / 256 * 256);
         p.chunk = std::min(T, most);
     }
-    p.cx = prec == TSID_BF16 ? 2 : 1;
+    p.cx = prec == TSID_BF16 ? TSID_SCORE_CX : 1;
     if (p.few) {
         p.n_tiles = 1;
         slices_of(n, 1, 2 * kCus, 128, 128, p.n_slices, p.slice_items);
     } else {
         const int64_t rows = 128 * p.cx;
         p.n_tiles = (int32_t)((p.chunk + rows - 1) / rows);
-        slices_of(n, p.n_tiles, 4 * kCus, 256, 64, p.n_slices, p.slice_items);
+        slices_of(n, p.n_tiles, TSID_SCORE_GRID * kCus, 256, 64, p.n_slices, p.slice_items);
     }
     p.part = c.take<float4>((int64_t)p.n_slices * p.chunk);
     if (top > 0) {
@@ -1052,7 +1114,7 @@ void launch_score(const ScoreK &a, const ScorePlan &p, hipStream_t s) {
     if (p.few) {
         k_score_few<K, NP, ENT><<<p.n_slices, kThreads, 0, s>>>(a);
     } else {
-        constexpr int CX = NP == 1 ? 2 : 1, YT = NP == 1 ? 64 : 32;
+        constexpr int CX = NP == 1 ? TSID_SCORE_CX : 1, YT = NP == 1 ? 64 : 32;
         constexpr size_t lds = 2 * Tile<K, NP, YT>::kBytes;
         static_assert(lds <= 64 * 1024, "within the default limit of dynamic LDS");
         k_score_pass<K, NP, CX, YT, ENT><<<grid_of(p.n_slices, a.n_tiles), kThreads, lds, s>>>(a);
@@ -1111,7 +1173,6 @@ void score_rows(const Head &h, const ScorePlan &p, FinishK f, bool entropy, hipS
     f.n_parts = p.n_slices;
     f.H = a.H;
     f.F = a.F;
-    f.k = h.k;
     f.scale = h.scale;
     f.bias_scale = h.bias_scale;
     f.blkmax = p.blkmax;
@@ -1128,12 +1189,16 @@ void score_rows(const Head &h, const ScorePlan &p, FinishK f, bool entropy, hipS
             else launch_score<kk(), np(), false>(a, p, s);
         });
         if (p.sup) {
-            k_block_groups<<<ceil_div(p.ngrp * a.T, kThreads), kThreads, 0, s>>>(p.blkmax, a.T, p.nblk, p.G, p.ngrp,
-                                                                                p.sup);
+            const int64_t row_tiles = (a.T + 31) / 32;
+            k_block_groups<<<(unsigned)(row_tiles * ((p.ngrp + 31) / 32)), kThreads, 0, s>>>(p.blkmax, a.T, p.nblk, p.G,
+                                                                                            p.ngrp, row_tiles, p.sup);
             TSID_HIP(hipGetLastError());
         }
-        if (h.prec == TSID_BF16) k_score_finish<uint16_t><<<(unsigned)a.T, kThreads, 0, s>>>(f);
-        else k_score_finish<float><<<(unsigned)a.T, kThreads, 0, s>>>(f);
+        for_rank(h.k, h.prec, [&](auto kk, auto np) {
+            using E = std::conditional_t<np() == 1, uint16_t, float>;
+            if (f.top > 0) k_score_finish<E, kk(), true><<<(unsigned)a.T, kThreads, 0, s>>>(f);
+            else k_score_finish<E, kk(), false><<<(unsigned)a.T, kThreads, 0, s>>>(f);
+        });
         TSID_HIP(hipGetLastError());
     }
 }
