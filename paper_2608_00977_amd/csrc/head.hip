@@ -17,6 +17,7 @@
 // Exponentials are base 2: p = 2^(c s - m) with c = |scale| log2 e (a negative
 // scale turns the sign of X).
 #include <algorithm>
+#include <atomic>
 #include <cmath>
 #include <type_traits>
 
@@ -26,15 +27,6 @@ namespace tsid {
 
 namespace {
 
-#ifndef TSID_SCORE_CX
-#define TSID_SCORE_CX 2
-#endif
-#ifndef TSID_SCORE_WAVES
-#define TSID_SCORE_WAVES 2
-#endif
-#ifndef TSID_SCORE_GRID
-#define TSID_SCORE_GRID 4
-#endif
 constexpr int kThreads = 256;
 constexpr double kLog2e = 1.4426950408889634074, kLn2 = 0.69314718055994530942;
 constexpr float kOff = -2e30f;    // the exponent's offset at an excluded item
@@ -130,30 +122,31 @@ struct Tile {
     static constexpr int kPer = (YT * S::CH + kThreads - 1) / kThreads;  // chunks per thread
     static constexpr size_t kBytes = (size_t)NP * kPlane * 2 + YT * 16;
     Raw<NP> raw[kPer];
-    float bias[kPer];
 
-    // Rows y0 .. y0 + YT - 1 into registers; zeros beyond the side and for excluded items.
+    static __device__ __forceinline__ bool idle(int q) { return (YT * S::CH) % kThreads != 0 && q >= YT * S::CH; }
+    // Rows y0 .. y0 + YT - 1 into registers (the side's last row beyond its end).
     __device__ __forceinline__ void load(const Side &Y, int64_t y0) {
 #pragma unroll
         for (int i = 0; i < kPer; ++i) {
             const int q = threadIdx.x + i * kThreads;
-            const int64_t row = y0 + q / S::CH;
-            raw[i] = zero_raw<NP>();
-            bias[i] = 0.f;
-            if ((YT * S::CH) % kThreads != 0 && q >= YT * S::CH) continue;
-            if (row < Y.count) {
-                raw[i] = load_raw<NP>(Y.p, row * Y.ld + (q % S::CH) * 8);
-                if (Y.bias) bias[i] = Y.bias[row];
-            }
+            if (idle(q)) continue;
+            const int64_t row = std::min<int64_t>(y0 + q / S::CH, Y.count - 1);
+            raw[i] = load_raw<NP>(Y.p, row * Y.ld + (q % S::CH) * 8);
         }
     }
-    __device__ __forceinline__ void store(const Side &Y, uint16_t *lds) const {
+    // ... into LDS; `special`: zeros for rows beyond the side and excluded items.
+    __device__ __forceinline__ void store(const Side &Y, int64_t y0, bool special, uint16_t *lds) const {
 #pragma unroll
         for (int i = 0; i < kPer; ++i) {
             const int q = threadIdx.x + i * kThreads;
-            if ((YT * S::CH) % kThreads != 0 && q >= YT * S::CH) continue;
+            if (idle(q)) continue;
+            Raw<NP> r = raw[i];
+            if (special) {
+                const int64_t row = y0 + q / S::CH;
+                if (row >= Y.count || (Y.bias && Y.bias[row] < kExcluded)) r = zero_raw<NP>();
+            }
             b8 part[NP];
-            parts_of<NP>(bias[i] < kExcluded ? zero_raw<NP>() : raw[i], part);
+            parts_of<NP>(r, part);
 #pragma unroll
             for (int p = 0; p < NP; ++p)
                 *reinterpret_cast<uint4 *>(lds + p * kPlane + (q / S::CH) * S::RS + (q % S::CH) * 8) =
@@ -238,12 +231,10 @@ __device__ __forceinline__ float take(Stat &st, const f16 &acc, float c, const f
         for (int r = 1; r < 16; ++r) top = fmaxf(top, acc[r]);
         top *= c;
     }
-    if (__any(top > st.m)) {
-        const float m = fmaxf(st.m, top), d = st.m - m, f = __builtin_amdgcn_exp2f(d);
-        if (ENT) st.e = fmaf(st.s, d, st.e) * f;
-        st.s *= f;
-        st.m = m;
-    }
+    const float m = fmaxf(st.m, top), d = st.m - m, f = __builtin_amdgcn_exp2f(d);
+    if (ENT) st.e = fmaf(st.s, d, st.e) * f;
+    st.s *= f;
+    st.m = m;
     float s0 = 0.f, s1 = 0.f, e0 = 0.f, e1 = 0.f;
 #pragma unroll
     for (int r = 0; r < 16; r += 2) {
@@ -272,8 +263,19 @@ struct ScoreK {
     int64_t slice_items;
     int32_t n_slices, n_tiles;
     float4 *part;      // [slice][T]: m, s, e
-    float *blkmax;     // [item / 32][T], or null
+    float *blkmax;     // [row / 64][item / 32][row % 64]: the largest score of each block of 32 items ([item / 32][T] for few rows)
+    int64_t nblk;
+    float *sup;        // [T][ngrp]: of each group of 2^g_log blocks, or null
+    int32_t g_log;
+    int64_t ngrp;
 };
+
+// In lanes 0 .. 31 the larger of a lane's a and lane + 32's; in the others the
+// same of b, with lane - 32's.
+__device__ __forceinline__ float max_halves(float a, float b) {
+    const auto p = __builtin_amdgcn_permlane32_swap(__float_as_uint(a), __float_as_uint(b), false, false);
+    return fmaxf(__uint_as_float(p[0]), __uint_as_float(p[1]));
+}
 
 // The slice and row tile of a workgroup: workgroups go to the 8 XCDs in turn,
 // so that the row tiles which read a slice of F run on one XCD and share its L2.
@@ -292,81 +294,122 @@ inline int grid_of(int32_t n_slices, int32_t n_tiles) {
     return n_slices < 8 ? n_slices * n_tiles : (n_slices + 7) / 8 * 8 * n_tiles;
 }
 
-// Many rows: four waves of CX * 32 rows each share tiles of F through LDS, two
-// tiles deep (one is read while the next one's loads are in flight).
-template <int K, int NP, int CX, int YT, bool ENT>
-__global__ __launch_bounds__(kThreads, TSID_SCORE_WAVES) void k_score_pass(ScoreK A) {
+// Many rows: four waves of CX * 32 rows each share tiles of F through LDS, three
+// tiles deep: while one is worked on, the next is there (its first scores are
+// taken already) and the one after it is on its way from memory.  The matrix
+// products of 32 items run beside the exponentials of the 32 before them: both
+// are in one stretch of code without branches, dealt out in turn.
+template <int K, int NP, int CX, int YT, bool ENT, bool TOP>
+__global__ __launch_bounds__(kThreads, 2) void k_score_pass(ScoreK A) {
     using TL = Tile<K, NP, YT>;
+    using S = Shape<K, NP>;
     extern __shared__ __align__(16) unsigned char smem[];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, h = lane >> 5;
     int32_t slice, tile;
     if (!place(A.n_slices, A.n_tiles, slice, tile)) return;
-    const int64_t x0 = A.t0 + (int64_t)tile * (4 * CX * 32) + wave * (CX * 32);
+    const int64_t x0 = (int64_t)tile * (4 * CX * 32) + wave * (CX * 32);  // of this run's rows
     const int64_t i0 = slice * A.slice_items, i1 = std::min<int64_t>(i0 + A.slice_items, A.F.count);
     auto buf = [&](int b) { return reinterpret_cast<uint16_t *>(smem + b * TL::kBytes); };
     if constexpr (K < 32) {
-        for (size_t j = threadIdx.x; j < 2 * TL::kBytes / 4; j += kThreads) reinterpret_cast<uint32_t *>(smem)[j] = 0u;
+        for (size_t j = threadIdx.x; j < 3 * TL::kBytes / 4; j += kThreads) reinterpret_cast<uint32_t *>(smem)[j] = 0u;
         __syncthreads();
     }
-    b8 x[CX][Shape<K, NP>::KS][NP];
+    b8 x[CX][S::KS][NP];
     const Side X{A.H.p, A.t0 + A.T, A.H.ld, nullptr};
 #pragma unroll
-    for (int q = 0; q < CX; ++q) load_x<K, NP>(X, x0 + 32 * q, A.turn, x[q]);
+    for (int q = 0; q < CX; ++q) load_x<K, NP>(X, A.t0 + x0 + 32 * q, A.turn, x[q]);
     Stat st[CX];
+    float group = kOff;
+    auto special = [&](int64_t y0) { return A.F.bias != nullptr || y0 + YT > i1; };
     TL t;
-    auto put = [&](uint16_t *b, int64_t y0) {
-        t.store(A.F, b);
-        if (threadIdx.x < YT) {
+    auto put = [&](int b, int64_t y0) {
+        const bool sp = special(y0);
+        t.store(A.F, y0, sp, buf(b));
+        if (sp && threadIdx.x < YT) {
             const int64_t i = y0 + threadIdx.x;
             float o = kOff;
             if (i < i1) {
                 o = A.F.bias ? A.F.bias[i] : 0.f;
                 o = o < kExcluded ? kOff : o * A.bias_c;
             }
-            reinterpret_cast<float *>(b + NP * TL::kPlane)[threadIdx.x] = o;
+            reinterpret_cast<float *>(buf(b) + NP * TL::kPlane)[threadIdx.x] = o;
         }
     };
-    int cur = 0;
-    t.load(A.F, i0);
-    put(buf(0), i0);
-    __syncthreads();
-    for (int64_t y0 = i0; y0 < i1; y0 += YT) {
-        const bool more = y0 + YT < i1;
-        if (more) t.load(A.F, y0 + YT);
-        const uint16_t *b = buf(cur);
-        const float *off = reinterpret_cast<const float *>(b + NP * TL::kPlane) + 4 * h;
-        const bool masked = A.F.bias || y0 + YT > i1;
+    if (i0 < i1) {
+        t.load(A.F, i0);
+        put(0, i0);
+        t.load(A.F, i0 + YT);
+        put(1, i0 + YT);
+        __syncthreads();
+        f16 acc[CX];
 #pragma unroll
-        for (int u = 0; u < YT / 32; ++u) {
-            f16 acc[CX];
+        for (int q = 0; q < CX; ++q) acc[q] = scores<K, NP, YT>(buf(0), x[q]);
+        int cur = 0;
+        auto work = [&](int64_t y0, const uint16_t *b, const uint16_t *b_next, auto masked) {
+            const float *off = reinterpret_cast<const float *>(b + NP * TL::kPlane) + 4 * h;
 #pragma unroll
-            for (int q = 0; q < CX; ++q) acc[q] = scores<K, NP, YT>(b + u * 32 * Shape<K, NP>::RS, x[q]);
-            float top[CX];
-            if (masked) {
+            for (int u = 0; u < YT / 32; ++u) {
+                const uint16_t *y = u + 1 < YT / 32 ? b + (u + 1) * 32 * S::RS : b_next;
+                f16 next[CX];
+                float top[CX];
+                if constexpr (masked()) {  // a tile now and then, or a biased table: one after the other, in fewer registers
 #pragma unroll
-                for (int q = 0; q < CX; ++q) top[q] = take<ENT, true>(st[q], acc[q], A.c, off + 32 * u);
-            } else {
+                    for (int q = 0; q < CX; ++q) top[q] = take<ENT, true>(st[q], acc[q], A.c, off + 32 * u);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
 #pragma unroll
-                for (int q = 0; q < CX; ++q) top[q] = take<ENT, false>(st[q], acc[q], A.c, nullptr);
+                for (int q = 0; q < CX; ++q) next[q] = scores<K, NP, YT>(y, x[q]);
+                if constexpr (!masked()) {
+#pragma unroll
+                    for (int q = 0; q < CX; ++q) top[q] = take<ENT, false>(st[q], acc[q], A.c, nullptr);
+                    constexpr int kProducts = CX * S::KS * (NP == 1 ? 1 : 6), kVector = CX * (ENT ? 76 : 60);
+#pragma unroll
+                    for (int g = 0; g < kProducts; ++g) {
+                        __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);  // a matrix product, then its share of vector work
+                        __builtin_amdgcn_sched_group_barrier(0x2, (kVector + kProducts - 1) / kProducts, 0);
+                    }
+                }
+                if constexpr (TOP) {
+                    // both halves of a wave join; lanes 32 and up then hold the
+                    // second 32 rows (CX = 2), so that the store needs no branch,
+                    // whose wait would hold up the loads of the tile to come
+                    if (!masked() || y0 + 32 * u < i1) {
+                        const int64_t blk = (y0 >> 5) + u;
+                        const float v = max_halves(top[0], top[CX - 1]);
+                        const int32_t row = (int32_t)x0 + (CX == 2 ? lane : lane & 31);
+                        // (a wave's values follow one another in memory)
+                        A.blkmax[((int64_t)(row >> 6) * A.nblk + blk) * 64 + (row & 63)] = v;
+                        group = fmaxf(group, v);
+                    }
+                }
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int q = 0; q < CX; ++q) acc[q] = next[q];
             }
-            if (A.blkmax && y0 + 32 * u < i1) {
-#pragma unroll
-                for (int q = 0; q < CX; ++q) {
-                    const float v = fmaxf(top[q], __shfl_xor(top[q], 32, 64));
-                    const int64_t row = x0 - A.t0 + 32 * q + (lane & 31);
-                    if (h == 0 && row < A.T) A.blkmax[((y0 + 32 * u) >> 5) * A.T + row] = v;
+        };
+        for (int64_t y0 = i0; y0 < i1; y0 += YT) {
+            const int nxt = cur == 2 ? 0 : cur + 1, far = nxt == 2 ? 0 : nxt + 1;
+            t.load(A.F, y0 + 2 * YT);
+            if (special(y0)) work(y0, buf(cur), buf(nxt), std::true_type());
+            else work(y0, buf(cur), buf(nxt), std::false_type());
+            if constexpr (TOP) {
+                const int64_t end = y0 + YT;  // of whole groups, or of the items
+                if (A.sup && ((end & ((32 << A.g_log) - 1)) == 0 || end >= A.F.count)) {
+                    const int64_t row = x0 + (CX == 2 ? lane : lane & 31);
+                    if (row < A.T) A.sup[row * A.ngrp + ((end - 1) >> (5 + A.g_log))] = group;
+                    group = kOff;
                 }
             }
+            put(far, y0 + 2 * YT);
+            __syncthreads();
+            cur = nxt;
         }
-        if (more) put(buf(cur ^ 1), y0 + YT);
-        __syncthreads();
-        cur ^= 1;
     }
 #pragma unroll
     for (int q = 0; q < CX; ++q) {
         Stat o{__shfl_xor(st[q].m, 32, 64), __shfl_xor(st[q].s, 32, 64), __shfl_xor(st[q].e, 32, 64)};
         merge(st[q], o);
-        const int64_t row = x0 - A.t0 + 32 * q + (lane & 31);
+        const int64_t row = x0 + 32 * q + (lane & 31);
         if (h == 0 && row < A.T) A.part[(int64_t)slice * A.T + row] = make_float4(st[q].m, st[q].s, st[q].e, 0.f);
     }
 }
@@ -376,6 +419,7 @@ __global__ __launch_bounds__(kThreads, TSID_SCORE_WAVES) void k_score_pass(Score
 // lines are read by two to four loads that follow one another).
 template <int K, int NP, bool ENT>
 __global__ __launch_bounds__(kThreads, 2) void k_score_few(ScoreK A) {
+    // a wave's items are contiguous, whole groups of blocks where there are groups
     using S = Shape<K, NP>;
     __shared__ float4 join[4][32];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, h = lane >> 5;
@@ -384,7 +428,9 @@ __global__ __launch_bounds__(kThreads, 2) void k_score_few(ScoreK A) {
     b8 x[S::KS][NP];
     load_x<K, NP>(Side{A.H.p, A.t0 + A.T, A.H.ld, nullptr}, A.t0, A.turn, x);
     Stat st;
-    for (int64_t y0 = i0 + wave * 32; y0 < i1; y0 += 128) {
+    float group = kOff;
+    const int64_t w0 = i0 + wave * (A.slice_items / 4), w1 = std::min<int64_t>(w0 + A.slice_items / 4, i1);
+    for (int64_t y0 = w0; y0 < w1; y0 += 32) {
         const int64_t item = y0 + (lane & 31);
         float o = kOff;
         if (item < i1) {
@@ -415,8 +461,14 @@ __global__ __launch_bounds__(kThreads, 2) void k_score_few(ScoreK A) {
             top = take<ENT, false>(st, acc, A.c, nullptr);
         }
         if (A.blkmax) {
-            const float v = fmaxf(top, __shfl_xor(top, 32, 64));
-            if (lane < A.T) A.blkmax[(y0 >> 5) * A.T + lane] = v;
+            const int64_t blk = y0 >> 5;
+            const float v = max_halves(top, top);
+            if (lane < A.T) A.blkmax[blk * A.T + lane] = v;
+            group = fmaxf(group, v);
+            if (A.sup && (((blk + 1) & ((1 << A.g_log) - 1)) == 0 || y0 + 32 >= A.F.count)) {
+                if (lane < A.T) A.sup[lane * A.ngrp + (blk >> A.g_log)] = group;
+                group = kOff;
+            }
         }
     }
     Stat o{__shfl_xor(st.m, 32, 64), __shfl_xor(st.s, 32, 64), __shfl_xor(st.e, 32, 64)};
@@ -430,32 +482,13 @@ __global__ __launch_bounds__(kThreads, 2) void k_score_few(ScoreK A) {
     }
 }
 
-// sup[t][g] = the largest of blkmax[b][t] over the G blocks of group g: tiles
-// of 32 rows and 32 groups, turned through LDS, so that both sides move lines.
-__global__ __launch_bounds__(kThreads) void k_block_groups(const float *blkmax, int64_t T, int64_t nblk, int64_t G,
-                                                           int64_t ngrp, int64_t row_tiles, float *sup) {
-    __shared__ float turn[32][33];
-    const int x = threadIdx.x & 31, y = threadIdx.x >> 5;
-    const int64_t t0 = blockIdx.x % row_tiles * 32, g0 = blockIdx.x / row_tiles * 32;
-    for (int q = y; q < 32; q += kThreads / 32) {
-        const int64_t b0 = (g0 + q) * G, b1 = std::min<int64_t>(b0 + G, nblk);
-        float v = kOff;
-        if (t0 + x < T)
-            for (int64_t b = b0; b < b1; ++b) v = fmaxf(v, blkmax[b * T + t0 + x]);
-        turn[q][x] = v;
-    }
-    __syncthreads();
-    for (int q = y; q < 32; q += kThreads / 32)
-        if (t0 + q < T && g0 + x < ngrp) sup[(t0 + q) * ngrp + g0 + x] = turn[x][q];
-}
-
 // ------------------------------------------------- a row's results
 
 constexpr int kMargin = 8;        // blocks beyond the wanted best items that are looked at
 constexpr int kMaxPick = TSID_MAX_TOP + kMargin;
-constexpr int kSelCap = 2048;     // candidates chosen from at a time
-constexpr int kMaxGroups = 2048;  // one round of them
-constexpr int kCandBytes = kMaxPick * 32 * 8 > kSelCap * 8 ? kMaxPick * 32 * 8 : kSelCap * 8;
+constexpr int kSelCap = kMaxPick * 32;  // candidates chosen from at a time: the items of the picked blocks
+constexpr int kMaxGroups = 2048;        // one round of them
+static_assert(kMaxGroups <= kSelCap && kMaxPick <= kThreads, "");
 
 // Larger floats have larger keys; NaN is below everything.
 __device__ __forceinline__ uint32_t order_key(float v) {
@@ -470,107 +503,54 @@ __device__ __forceinline__ uint64_t order_key(double v) {
 }
 
 struct SelectLds {
-    uint32_t hist[256], wsum[4];
-    uint32_t digit, need, count, found;
-    int32_t place[kThreads];
+    uint32_t best[kThreads];
+    uint32_t found;
+    uint16_t place[kSelCap];
+    int32_t out[kMaxPick];
 };
 
-// Sum over the threads before this one of the 256, and all of them.
-__device__ __forceinline__ uint32_t before(uint32_t v, uint32_t *wsum, uint32_t &total) {
-    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-    uint32_t incl = v;
-#pragma unroll
-    for (int off = 1; off < 64; off <<= 1) {
-        const uint32_t o = __shfl_up(incl, off, 64);
-        if (lane >= off) incl += o;
-    }
-    __syncthreads();
-    if (lane == 63) wsum[w] = incl;
-    __syncthreads();
-    uint32_t pre = 0;
-    total = 0;
-    for (int q = 0; q < 4; ++q) {
-        if (q < w) pre += wsum[q];
-        total += wsum[q];
-    }
-    return pre + incl - v;
-}
-
-// The `want` (at most kMaxPick) largest of key[0 .. N - 1], equal keys in
-// order of place: returns in thread j < min(want, N) the place of the j-th, and
-// -1 elsewhere.  The keys' digits are gone through from the top until no more
-// than 256 keys can still be among them, which are then ranked by counting;
-// only where more are equal to the last bit are the first of them taken.
-template <typename U>
-__device__ int32_t select_largest(const U *key, int N, int want, SelectLds &L) {
-    const int t = threadIdx.x;
+// The `want` (at most kMaxPick) largest of key[0 .. N - 1] (N <= kSelCap), equal
+// keys in order of place: thread j < min(want, N) returns the place of the
+// j-th, the others -1.  Of the best upper half of each thread's share the
+// want-th largest is a bound that at least `want` keys reach (found bit by
+// bit, every wave for itself); the keys that reach it, hardly more, are ranked
+// by counting.
+__device__ int32_t select_largest(const uint64_t *key, int N, int want, SelectLds &L) {
+    const int t = threadIdx.x, lane = t & 63;
     if (want > N) want = N;
-    int have = N;
-    if (N <= kThreads) {
-        if (t < N) L.place[t] = t;
-        __syncthreads();
-    } else {
-        U prefix = 0, mask = 0;
-        uint32_t need = (uint32_t)want, left = (uint32_t)N;
-        for (int shift = (int)sizeof(U) * 8 - 8; shift >= 0 && left > (uint32_t)kThreads; shift -= 8) {
-            L.hist[t] = 0u;
-            __syncthreads();
-            for (int j = t; j < N; j += kThreads)
-                if ((key[j] & mask) == prefix) atomicAdd(&L.hist[(uint32_t)(key[j] >> shift) & 255u], 1u);
-            __syncthreads();
-            uint32_t total;
-            const uint32_t mine = L.hist[255 - t];  // thread t: digit 255 - t
-            const uint32_t above = before(mine, L.wsum, total);
-            if (above < need && need <= above + mine) {
-                L.digit = 255u - t;
-                L.need = need - above;
-                L.count = mine;
-            }
-            __syncthreads();
-            prefix |= (U)L.digit << shift;
-            mask |= (U)255u << shift;
-            need = L.need;
-            left = (uint32_t)want - need + L.count;
-            __syncthreads();
-        }
-        if (left <= (uint32_t)kThreads) {
-            if (t == 0) L.found = 0u;
-            __syncthreads();
-            for (int j = t; j < N; j += kThreads)
-                if ((key[j] & mask) >= prefix) L.place[atomicAdd(&L.found, 1u)] = j;
-            have = (int)left;
-        } else {  // the first `need` of the keys equal to prefix
-            const int per = (N + kThreads - 1) / kThreads, j0 = t * per, j1 = j0 + per < N ? j0 + per : N;
-            uint32_t eq = 0, take = 0, total;
-            for (int j = j0; j < j1; ++j) eq += key[j] == prefix;
-            const uint32_t eq_before = before(eq, L.wsum, total);
-            uint32_t e = eq_before;
-            for (int j = j0; j < j1; ++j) take += key[j] > prefix || (key[j] == prefix && e++ < need);
-            uint32_t at = before(take, L.wsum, total);
-            e = eq_before;
-            for (int j = j0; j < j1; ++j)
-                if (key[j] > prefix || (key[j] == prefix && e++ < need)) L.place[at++] = j;
-            have = want;
-        }
-        __syncthreads();
+    uint32_t best = 0u;
+    for (int j = t; j < N; j += kThreads) best = max(best, (uint32_t)(key[j] >> 32));
+    L.best[t] = best;
+    if (t == 0) L.found = 0u;
+    __syncthreads();
+    uint32_t four[4], bound = 0u;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) four[q] = L.best[64 * q + lane];
+    for (int bit = 31; bit >= 0; --bit) {
+        const uint32_t with = bound | 1u << bit;
+        int reach = 0;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) reach += __popcll(__ballot(four[q] >= with));
+        if (reach >= want) bound = with;
     }
-    int rank = kThreads;
-    int32_t mine = 0;
-    if (t < have) {
-        mine = L.place[t];
-        const U k = key[mine];
-        rank = 0;
+    for (int j = t; j < N; j += kThreads) {
+        if ((uint32_t)(key[j] >> 32) >= bound) L.place[atomicAdd(&L.found, 1u)] = (uint16_t)j;
+    }
+    __syncthreads();
+    const int have = (int)L.found;
+    for (int q = t; q < have; q += kThreads) {
+        const int32_t p = L.place[q];
+        const uint64_t k = key[p];
+        int rank = 0;
+#pragma unroll 8
         for (int j = 0; j < have; ++j) {
-            const int32_t p = L.place[j];
-            rank += key[p] > k || (key[p] == k && p < mine);
+            const int32_t o = L.place[j];
+            rank += key[o] > k || (key[o] == k && o < p);
         }
+        if (rank < want) L.out[rank] = p;
     }
     __syncthreads();
-    if (rank < want) L.place[rank] = mine;
-    __syncthreads();
-    const int32_t out = t < want ? L.place[t] : -1;
-    __syncthreads();
-    return out;
+    return t < want ? L.out[t] : -1;
 }
 
 struct FinishK {
@@ -587,7 +567,8 @@ struct FinishK {
     float *loss;
     int32_t top;
     const float *blkmax, *sup;
-    int64_t nblk, G, ngrp;
+    int64_t nblk, ngrp;
+    int32_t g_log, width;  // rows that lie together in blkmax
     int32_t *top_ids;
     float *top_logp;
     int32_t *err;
@@ -600,6 +581,15 @@ __device__ __forceinline__ f8 load8(const float *p) {
 }
 __device__ __forceinline__ f8 load8(const uint16_t *p) {
     return __builtin_convertvector(__builtin_bit_cast(b8, *reinterpret_cast<const uint4 *>(p)), f8);
+}
+
+// The value of another lane of the same 16, by a data-parallel move.
+template <int CTRL>
+__device__ __forceinline__ double across(double v) {
+    const uint64_t b = (uint64_t)__double_as_longlong(v);
+    const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)b, CTRL, 0xF, 0xF, true);
+    const uint32_t hi = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)(b >> 32), CTRL, 0xF, 0xF, true);
+    return __longlong_as_double((long long)((uint64_t)hi << 32 | lo));
 }
 
 __device__ __forceinline__ double block_sum(double v, double *red) {
@@ -659,8 +649,10 @@ __global__ __launch_bounds__(kThreads) void k_score_finish(FinishK A) {
         double z = 0.0;
 #pragma unroll
         for (int c = 0; c < 8; ++c) z = fma((double)hv[c], (double)f[c], z);
-#pragma unroll
-        for (int off = LN / 2; off > 0; off >>= 1) z += __shfl_xor(z, off, LN);
+        if constexpr (LN >= 2) z += across<0xB1>(z);    // lanes i ^ 1
+        if constexpr (LN >= 4) z += across<0x4E>(z);    // i ^ 2
+        if constexpr (LN >= 8) z += across<0x141>(z);   // 7 - i of each 8
+        if constexpr (LN >= 16) z += across<0x140>(z);  // 15 - i of each 16
         return z * A.scale + (A.F.bias ? (double)A.F.bias[id] * A.bias_scale : 0.0);
     };
     const int32_t *ids = A.ids ? A.ids + t * A.per_row : nullptr;
@@ -701,12 +693,11 @@ __global__ __launch_bounds__(kThreads) void k_score_finish(FinishK A) {
         if (tid == 0) A.loss[t] = w_sum > 0.0 ? (float)(A.tau * A.tau * (a_sum / w_sum - log(w_sum))) : 0.f;
     }
     if constexpr (TOP) {
-        __shared__ __align__(16) unsigned char cand[kCandBytes];
+        __shared__ uint64_t cand[kSelCap];
         __shared__ int32_t pick[2][kMaxPick];
         __shared__ SelectLds L;
-        uint32_t *key = reinterpret_cast<uint32_t *>(cand);
-        int32_t *pay = reinterpret_cast<int32_t *>(cand + kSelCap * 4);
-        // the `want` largest of `total` candidates get(j, value, payload), best first, to out
+        // the `want` largest of `total` candidates get(j, value, payload), equal
+        // ones in order of payload, best first, to out
         auto choose = [&](int64_t total, int want, int32_t *out, auto get) {
             int have = 0;
             int64_t next = 0;
@@ -716,24 +707,17 @@ __global__ __launch_bounds__(kThreads) void k_score_finish(FinishK A) {
                     float v;
                     int32_t p;
                     get(next + j, v, p);
-                    key[have + j] = order_key(v);
-                    pay[have + j] = p;
+                    cand[have + j] = (uint64_t)order_key(v) << 32 | (uint32_t)~p;
                 }
                 __syncthreads();
                 next += n_new;
-                const int32_t place = select_largest(key, have + n_new, want, L);
+                const int32_t place = select_largest(cand, have + n_new, want, L);
                 have = std::min(have + n_new, want);
-                uint32_t k0 = 0;
-                int32_t p0 = 0;
-                if (place >= 0) {
-                    k0 = key[place];
-                    p0 = pay[place];
-                }
+                const uint64_t c = place >= 0 ? cand[place] : 0;
                 __syncthreads();
                 if (place >= 0) {  // the front of the next round
-                    key[tid] = k0;
-                    pay[tid] = p0;
-                    out[tid] = p0;
+                    cand[tid] = c;
+                    out[tid] = (int32_t)~(uint32_t)c;
                 }
                 __syncthreads();
             } while (next < total);
@@ -741,30 +725,21 @@ __global__ __launch_bounds__(kThreads) void k_score_finish(FinishK A) {
         };
         const int want = A.top + kMargin;
         int got;
+        const float *maxima = A.blkmax + row / A.width * A.nblk * A.width + row % A.width;
         if (A.sup) {
             const float *sup = A.sup + row * A.ngrp;
             const int groups = choose(A.ngrp, want, pick[0], [&](int64_t j, float &v, int32_t &p) {
                 v = sup[j];
                 p = (int32_t)j;
             });
-            // in ascending order of blocks, for the ties
-            int32_t g = 0;
-            int rank = 0;
-            if (tid < groups) {
-                g = pick[0][tid];
-                for (int j = 0; j < groups; ++j) rank += pick[0][j] < g;
-            }
-            __syncthreads();
-            if (tid < groups) pick[0][rank] = g;
-            __syncthreads();
-            got = choose(groups * A.G, want, pick[1], [&](int64_t j, float &v, int32_t &p) {
-                const int64_t b = pick[0][j / A.G] * A.G + j % A.G;
-                v = b < A.nblk ? A.blkmax[b * A.T + row] : -INFINITY;
+            got = choose((int64_t)groups << A.g_log, want, pick[1], [&](int64_t j, float &v, int32_t &p) {
+                const int64_t b = ((int64_t)pick[0][j >> A.g_log] << A.g_log) + (j & ((1 << A.g_log) - 1));
+                v = b < A.nblk ? maxima[b * A.width] : -INFINITY;
                 p = (int32_t)b;
             });
         } else {
             got = choose(A.nblk, want, pick[1], [&](int64_t j, float &v, int32_t &p) {
-                v = A.blkmax[j * A.T + row];
+                v = maxima[j * A.width];
                 p = (int32_t)j;
             });
         }
@@ -778,8 +753,7 @@ __global__ __launch_bounds__(kThreads) void k_score_finish(FinishK A) {
         __syncthreads();
         if (tid < got) pick[0][rank] = b0;  // ascending, for the ties
         __syncthreads();
-        uint64_t *key64 = reinterpret_cast<uint64_t *>(cand);
-        constexpr int U = 4;  // items of a lane group in flight
+        constexpr int U = 8;  // items of a lane group in flight
         for (int j0 = tid / LN; j0 < got * 32; j0 += NI * U) {
             f8 f[U];
             int64_t id[U];
@@ -794,15 +768,15 @@ __global__ __launch_bounds__(kThreads) void k_score_finish(FinishK A) {
             for (int u = 0; u < U; ++u) {
                 const int j = j0 + u * NI;
                 const double z = score_of(std::max<int64_t>(id[u], 0), f[u]);
-                if (sub == 0 && j < got * 32) key64[j] = id[u] >= 0 ? order_key(z) : 0ull;
+                if (sub == 0 && j < got * 32) cand[j] = id[u] >= 0 ? order_key(z) : 0ull;
             }
         }
         __syncthreads();
-        const int32_t place = select_largest(key64, got * 32, A.top, L);
+        const int32_t place = select_largest(cand, got * 32, A.top, L);
         if (tid < A.top) {
             int32_t id = -1;
             float lp = -INFINITY;
-            const uint64_t kv = place >= 0 ? key64[place] : 0ull;
+            const uint64_t kv = place >= 0 ? cand[place] : 0ull;
             if (kv != 0ull) {
                 id = pick[0][place >> 5] * 32 + (place & 31);
                 const double z = __longlong_as_double((long long)((kv >> 63) ? kv & ~(1ull << 63) : ~kv));
@@ -927,7 +901,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_grad_pass(GradK A) {
     TL t;
     // a row of Y: the offset; ITEMS: its a and b
     auto put = [&](uint16_t *b, int64_t y0) {
-        t.store(A.Y, b);
+        t.store(A.Y, y0, (!ITEMS && A.Y.bias) || y0 + YT > A.Y.count, b);
         if (threadIdx.x < YT) {
             const int64_t i = y0 + threadIdx.x;
             float *o = reinterpret_cast<float *>(b + NP * TL::kPlane) + threadIdx.x;
@@ -949,8 +923,10 @@ __global__ __launch_bounds__(kThreads, 2) void k_grad_pass(GradK A) {
     };
     const int grp = lane >> 4, gi = lane & 15;
     int cur = 0;
-    t.load(A.Y, i0);
-    put(buf(0), i0);
+    if (i0 < i1) {  // nothing to read of an empty side
+        t.load(A.Y, i0);
+        put(buf(0), i0);
+    }
     __syncthreads();
     for (int64_t y0 = i0; y0 < i1; y0 += YT) {
         const bool more = y0 + YT < i1;
@@ -1072,7 +1048,8 @@ void slices_of(int64_t rows, int64_t tiles, int64_t wanted, int64_t least, int64
 struct ScorePlan {
     bool few;
     int64_t chunk;        // rows of a run
-    int64_t nblk, G, ngrp;
+    int64_t nblk, padded, ngrp;  // padded: rows with room in blkmax
+    int32_t g_log;
     int32_t n_slices, n_tiles, cx;
     int64_t slice_items;
     float4 *part;
@@ -1088,25 +1065,53 @@ ScorePlan plan_score(int64_t T, int64_t n, int prec, int top, Carve &c) {
         const int64_t most = std::max<int64_t>(256, (int64_t(1) << 28) / std::max<int64_t>(p.nblk, 1) / 256 * 256);
         p.chunk = std::min(T, most);
     }
-    p.cx = prec == TSID_BF16 ? TSID_SCORE_CX : 1;
+    p.cx = prec == TSID_BF16 ? 2 : 1;
+    if (top > 0)
+        while (p.g_log < 6 && p.nblk > (int64_t)kMaxGroups << p.g_log) ++p.g_log;
+    const int64_t G = int64_t(1) << p.g_log;  // blocks of a group
+    p.ngrp = (p.nblk + G - 1) / G;
+    p.padded = T;
     if (p.few) {
         p.n_tiles = 1;
-        slices_of(n, 1, 2 * kCus, 128, 128, p.n_slices, p.slice_items);
+        slices_of(n, 1, 2 * kCus, 128, 128 * G, p.n_slices, p.slice_items);
     } else {
         const int64_t rows = 128 * p.cx;
         p.n_tiles = (int32_t)((p.chunk + rows - 1) / rows);
-        slices_of(n, p.n_tiles, TSID_SCORE_GRID * kCus, 256, 64, p.n_slices, p.slice_items);
+        p.padded = p.n_tiles * rows;
+        slices_of(n, p.n_tiles, 4 * kCus, 256, std::max<int64_t>(64, 32 * G), p.n_slices, p.slice_items);
     }
     p.part = c.take<float4>((int64_t)p.n_slices * p.chunk);
     if (top > 0) {
-        p.blkmax = c.take<float>(p.nblk * p.chunk);
-        if (p.nblk > kMaxGroups) {
-            p.G = (p.nblk + kMaxGroups - 1) / kMaxGroups;
-            p.ngrp = (p.nblk + p.G - 1) / p.G;
-            p.sup = c.take<float>(p.ngrp * p.chunk);
-        }
+        p.blkmax = c.take<float>(p.nblk * p.padded);
+        if (p.g_log > 0) p.sup = c.take<float>(p.ngrp * p.chunk);
     }
     return p;
+}
+
+// Lets a kernel take `lds` bytes of dynamic LDS; `done`: a bit per device.
+void allow_lds(const void *kernel, size_t lds, std::atomic<uint64_t> &done) {
+    int device = 0;
+    TSID_HIP(hipGetDevice(&device));
+    const uint64_t bit = uint64_t(1) << (device & 63);
+    if (done.load() & bit) return;
+    TSID_HIP(hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
+    done.fetch_or(bit);
+}
+
+// 64 rows per wave in bf16: two sets of products share each read of F's tile
+// (2,048 x 1 M, k = 128: 555 us; 32 rows: 647 us).  Tiles of 64 rows of F, but of
+// 32 where the blocks' maxima are kept, whose registers would spill otherwise
+// (880 and 992 us with the best 20).  fp32: 32 rows and tiles of 32, three parts each.
+template <int K, int NP, bool ENT, bool TOP>
+void launch_score_pass(const ScoreK &a, hipStream_t s) {
+    constexpr int CX = NP == 1 ? 2 : 1, YT = NP == 1 && !TOP ? 64 : 32;
+    constexpr size_t lds = 3 * Tile<K, NP, YT>::kBytes;
+    auto *pass = &k_score_pass<K, NP, CX, YT, ENT, TOP>;
+    if (lds > 64 * 1024) {  // more dynamic LDS than the default limit: said once per kernel and device
+        static std::atomic<uint64_t> done;
+        allow_lds(reinterpret_cast<const void *>(pass), lds, done);
+    }
+    pass<<<grid_of(a.n_slices, a.n_tiles), kThreads, lds, s>>>(a);
 }
 
 template <int K, int NP, bool ENT>
@@ -1114,10 +1119,8 @@ void launch_score(const ScoreK &a, const ScorePlan &p, hipStream_t s) {
     if (p.few) {
         k_score_few<K, NP, ENT><<<p.n_slices, kThreads, 0, s>>>(a);
     } else {
-        constexpr int CX = NP == 1 ? TSID_SCORE_CX : 1, YT = NP == 1 ? 64 : 32;
-        constexpr size_t lds = 2 * Tile<K, NP, YT>::kBytes;
-        static_assert(lds <= 64 * 1024, "within the default limit of dynamic LDS");
-        k_score_pass<K, NP, CX, YT, ENT><<<grid_of(p.n_slices, a.n_tiles), kThreads, lds, s>>>(a);
+        if (a.blkmax) launch_score_pass<K, NP, ENT, true>(a, s);
+        else launch_score_pass<K, NP, ENT, false>(a, s);
     }
     TSID_HIP(hipGetLastError());
 }
@@ -1169,6 +1172,11 @@ void score_rows(const Head &h, const ScorePlan &p, FinishK f, bool entropy, hipS
     a.n_slices = p.n_slices;
     a.part = p.part;
     a.blkmax = p.blkmax;
+    a.sup = p.sup;
+    a.nblk = p.nblk;
+    f.width = p.few ? (int32_t)h.H.count : 64;
+    a.g_log = f.g_log = p.g_log;
+    a.ngrp = p.ngrp;
     f.part = p.part;
     f.n_parts = p.n_slices;
     f.H = a.H;
@@ -1178,7 +1186,6 @@ void score_rows(const Head &h, const ScorePlan &p, FinishK f, bool entropy, hipS
     f.blkmax = p.blkmax;
     f.sup = p.sup;
     f.nblk = p.nblk;
-    f.G = p.G;
     f.ngrp = p.ngrp;
     for (int64_t t0 = 0; t0 < h.H.count; t0 += p.chunk) {
         a.t0 = f.t0 = t0;
@@ -1188,12 +1195,6 @@ void score_rows(const Head &h, const ScorePlan &p, FinishK f, bool entropy, hipS
             if (entropy) launch_score<kk(), np(), true>(a, p, s);
             else launch_score<kk(), np(), false>(a, p, s);
         });
-        if (p.sup) {
-            const int64_t row_tiles = (a.T + 31) / 32;
-            k_block_groups<<<(unsigned)(row_tiles * ((p.ngrp + 31) / 32)), kThreads, 0, s>>>(p.blkmax, a.T, p.nblk, p.G,
-                                                                                            p.ngrp, row_tiles, p.sup);
-            TSID_HIP(hipGetLastError());
-        }
         for_rank(h.k, h.prec, [&](auto kk, auto np) {
             using E = std::conditional_t<np() == 1, uint16_t, float>;
             if (f.top > 0) k_score_finish<E, kk(), true><<<(unsigned)a.T, kThreads, 0, s>>>(f);
