@@ -561,9 +561,12 @@ tsid_status tsid_lookup_grad(tsid_ctx *ctx, int32_t prec, int32_t k, const tsid_
  * and p_ti = exp z_ti / sum_i' exp z_ti'.
  *  H     T rows.   F  n rows.  Both below 2^31 rows.
  *  bias  DEVICE n floats or NULL (no bias); constant: it gets no gradient.  A
- *        bias below -1e20 (-inf, the lowest float) excludes its item: p is 0
+ *        bias below -1e7 (-inf, the lowest float) excludes its item: p is 0
  *        and its row of F is not used, whatever it holds.  Otherwise finite.
- *  scale any finite number.  temperature: from 1e-6 to 1e6.
+ *  scale, temperature: scale / temperature is 0 or from 1e-12 to 1e12 in size,
+ *        temperature from 1e-6 to 1e6.
+ * Scores (divided by the temperature) lie above -5e7: lower ones count as
+ * excluded.
  * Scores of a row all of whose items are excluded (or n = 0): log sum -inf,
  * entropy 0, no best items, gradients 0.  A NaN in a row of H reaches that
  * row's results.  Products of bf16 factors are exact and added in fp32; fp32

@@ -2799,7 +2799,8 @@ Head check_head(const tsid_head *h) {
     o.k = h->k;
     o.prec = h->prec;
     o.scale = h->scale / h->temperature;
-    if (!std::isfinite(o.scale)) fail(TSID_E_INVAL, "scale / temperature must be finite");
+    if (o.scale != 0.f && !(std::fabs(o.scale) >= 1e-12f && std::fabs(o.scale) <= 1e12f))
+        fail(TSID_E_INVAL, "scale / temperature must be 0 or from 1e-12 to 1e12 in size");
     o.bias_scale = 1.f / h->temperature;
     return o;
 }

@@ -29,8 +29,8 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr double kLog2e = 1.4426950408889634074, kLn2 = 0.69314718055994530942;
-constexpr float kOff = -2e30f;    // the exponent's offset at an excluded item
-constexpr float kLeast = -1e30f;  // a running maximum before the first item
+constexpr float kOff = -1e9f;    // the exponent of an excluded item
+constexpr float kLeast = -1e8f;  // a running maximum before the first item
 
 typedef float f4 __attribute__((ext_vector_type(4)));
 typedef float f8 __attribute__((ext_vector_type(8)));
@@ -155,17 +155,20 @@ struct Tile {
     }
 };
 
-// The rows x0 + l % 32 of X as B operands, turned if `turn`.
+// What becomes of X's sign: kTurn for a negative scale; kNone (X zero) for scale 0.
+enum Turn { kKeep = 0, kTurn = 1, kNone = 2 };
+
+// The rows x0 + l % 32 of X as B operands.
 template <int K, int NP>
-__device__ __forceinline__ void load_x(const Side &X, int64_t x0, bool turn, b8 (&x)[Shape<K, NP>::KS][NP]) {
+__device__ __forceinline__ void load_x(const Side &X, int64_t x0, int turn, b8 (&x)[Shape<K, NP>::KS][NP]) {
     const int lane = threadIdx.x & 63;
     const int64_t row = x0 + (lane & 31);
 #pragma unroll
     for (int s = 0; s < Shape<K, NP>::KS; ++s) {
         const int c = 16 * s + 8 * (lane >> 5);
         Raw<NP> r = zero_raw<NP>();
-        if (row < X.count && c < K && !(X.bias && X.bias[row] < kExcluded)) r = load_raw<NP>(X.p, row * X.ld + c);
-        if (turn) {
+        if (turn != kNone && row < X.count && c < K && !(X.bias && X.bias[row] < kExcluded)) r = load_raw<NP>(X.p, row * X.ld + c);
+        if (turn == kTurn) {
             const uint32_t f = NP == 1 ? 0x80008000u : 0x80000000u;
             for (auto &w : r.w) w = make_uint4(w.x ^ f, w.y ^ f, w.z ^ f, w.w ^ f);
         }
@@ -173,13 +176,22 @@ __device__ __forceinline__ void load_x(const Side &X, int64_t x0, bool turn, b8 
     }
 }
 
-// S = Y X^T for the 32 rows of Y at `y` in LDS.
+// The row of a tile's 32-row block that the matrix unit's row m is: the four
+// rows that a lane's scores r .. r + 3 belong to lie two apart, and with a row
+// stride of 4 banks more than a whole number of turns the 16 rows that a
+// transposing read takes (four by four) fall on banks of their own.
+__device__ __forceinline__ constexpr int block_row(int m) { return (m & 24) | (m & 3) << 1 | (m >> 2 & 1); }
+__device__ __forceinline__ constexpr int matrix_row(int row) { return (row & 24) | (row & 1) << 2 | (row >> 1 & 3); }
+
+// Where a tile's row has its offset.
+__device__ __forceinline__ int offset_place(int row) { return (row & ~31) | matrix_row(row & 31); }
+
+// S = Y X^T for the 32 rows of Y at `y` in LDS, from acc.
 template <int K, int NP, int YT>
-__device__ __forceinline__ f16 scores(const uint16_t *y, const b8 (&x)[Shape<K, NP>::KS][NP]) {
+__device__ __forceinline__ f16 scores(const uint16_t *y, const b8 (&x)[Shape<K, NP>::KS][NP], f16 acc) {
     using S = Shape<K, NP>;
     const int lane = threadIdx.x & 63;
-    const uint16_t *row = y + (lane & 31) * S::RS + 8 * (lane >> 5);
-    f16 acc = {};
+    const uint16_t *row = y + block_row(lane & 31) * S::RS + 8 * (lane >> 5);
 #pragma unroll
     for (int s = 0; s < S::KS; ++s) {
         b8 a[NP];
@@ -191,8 +203,22 @@ __device__ __forceinline__ f16 scores(const uint16_t *y, const b8 (&x)[Shape<K, 
     return acc;
 }
 
-// The row of a 32-row tile that a lane's r-th score belongs to (without 4 (l / 32)).
+// The matrix unit's row that a lane's r-th score belongs to (without 4 (l / 32)).
 __device__ __forceinline__ constexpr int tile_row(int r) { return 8 * (r / 4) + r % 4; }
+
+// A value per row of a block, as its scores lie (off: of the lane's first row;
+// kept in the order of the matrix unit's rows).
+// Given to scores() to start from, an offset per row of Y costs no arithmetic.
+__device__ __forceinline__ f16 per_row(const float *off) {
+    f16 v;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        const f4 o = *reinterpret_cast<const f4 *>(off + 8 * q);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[4 * q + j] = o[j];
+    }
+    return v;
+}
 
 // ------------------------------------------------------------------ scores
 
@@ -209,28 +235,13 @@ __device__ __forceinline__ void merge(Stat &a, const Stat &b) {
     a.m = m;
 }
 
-// Takes 16 scores; returns the largest exponent.  MASKED: off[r] is added
-// (the items' bias, kOff where excluded), else nothing.
-template <bool ENT, bool MASKED>
-__device__ __forceinline__ float take(Stat &st, const f16 &acc, float c, const float *off) {
-    float x[16];
-    float top;
-    if constexpr (MASKED) {
+// Takes 16 scores; returns the largest exponent.
+template <bool ENT>
+__device__ __forceinline__ float take(Stat &st, const f16 &acc, float c) {
+    float top = acc[0];
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            const f4 o = *reinterpret_cast<const f4 *>(off + 8 * q);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) x[4 * q + j] = fmaf(acc[4 * q + j], c, o[j]);
-        }
-        top = x[0];
-#pragma unroll
-        for (int r = 1; r < 16; ++r) top = fmaxf(top, x[r]);
-    } else {
-        top = acc[0];
-#pragma unroll
-        for (int r = 1; r < 16; ++r) top = fmaxf(top, acc[r]);
-        top *= c;
-    }
+    for (int r = 1; r < 16; ++r) top = fmaxf(top, acc[r]);
+    top *= c;
     const float m = fmaxf(st.m, top), d = st.m - m, f = __builtin_amdgcn_exp2f(d);
     if (ENT) st.e = fmaf(st.s, d, st.e) * f;
     st.s *= f;
@@ -238,8 +249,7 @@ __device__ __forceinline__ float take(Stat &st, const f16 &acc, float c, const f
     float s0 = 0.f, s1 = 0.f, e0 = 0.f, e1 = 0.f;
 #pragma unroll
     for (int r = 0; r < 16; r += 2) {
-        const float y0 = MASKED ? x[r] - st.m : fmaf(acc[r], c, -st.m);
-        const float y1 = MASKED ? x[r + 1] - st.m : fmaf(acc[r + 1], c, -st.m);
+        const float y0 = fmaf(acc[r], c, -st.m), y1 = fmaf(acc[r + 1], c, -st.m);
         const float p0 = __builtin_amdgcn_exp2f(y0), p1 = __builtin_amdgcn_exp2f(y1);
         s0 += p0;
         s1 += p1;
@@ -257,7 +267,7 @@ struct ScoreK {
     Side H, F;
     float c;           // |scale| log2 e
     int turn;
-    float bias_c;      // log2 e / temperature
+    float bias_c, off;  // a bias, and the offset of an excluded item, in units of the scores s
     int64_t t0;        // first row of this run
     int64_t T;         // rows of this run
     int64_t slice_items;
@@ -299,7 +309,7 @@ inline int grid_of(int32_t n_slices, int32_t n_tiles) {
 // taken already) and the one after it is on its way from memory.  The matrix
 // products of 32 items run beside the exponentials of the 32 before them: both
 // are in one stretch of code without branches, dealt out in turn.
-template <int K, int NP, int CX, int YT, bool ENT, bool TOP>
+template <int K, int NP, int CX, int YT, bool BIAS, bool ENT, bool TOP>
 __global__ __launch_bounds__(kThreads, 2) void k_score_pass(ScoreK A) {
     using TL = Tile<K, NP, YT>;
     using S = Shape<K, NP>;
@@ -320,19 +330,47 @@ __global__ __launch_bounds__(kThreads, 2) void k_score_pass(ScoreK A) {
     for (int q = 0; q < CX; ++q) load_x<K, NP>(X, A.t0 + x0 + 32 * q, A.turn, x[q]);
     Stat st[CX];
     float group = kOff;
-    auto special = [&](int64_t y0) { return A.F.bias != nullptr || y0 + YT > i1; };
     TL t;
     auto put = [&](int b, int64_t y0) {
-        const bool sp = special(y0);
-        t.store(A.F, y0, sp, buf(b));
-        if (sp && threadIdx.x < YT) {
+        const bool some = BIAS || y0 + YT > i1;  // of its rows are left out, or have a bias
+        t.store(A.F, y0, some, buf(b));
+        if (some && threadIdx.x < YT) {
             const int64_t i = y0 + threadIdx.x;
-            float o = kOff;
+            float o = A.off;
             if (i < i1) {
-                o = A.F.bias ? A.F.bias[i] : 0.f;
-                o = o < kExcluded ? kOff : o * A.bias_c;
+                o = BIAS ? A.F.bias[i] : 0.f;
+                o = o < kExcluded ? A.off : o * A.bias_c;
             }
-            reinterpret_cast<float *>(buf(b) + NP * TL::kPlane)[threadIdx.x] = o;
+            reinterpret_cast<float *>(buf(b) + NP * TL::kPlane)[offset_place(threadIdx.x)] = o;
+        }
+    };
+    // the scores of block u of a tile
+    auto start = [&](const uint16_t *b, int u, f16 (&acc)[CX], auto offsets) {
+        const float *off = reinterpret_cast<const float *>(b + NP * TL::kPlane) + 32 * u + 4 * h;
+#pragma unroll
+        for (int q = 0; q < CX; ++q)
+            acc[q] = scores<K, NP, YT>(b + u * 32 * S::RS, x[q], offsets() ? per_row(off) : f16{});
+    };
+    // keeps the largest scores of the block at item y
+    auto keep = [&](const float (&top)[CX], int64_t y) {
+        if constexpr (TOP) {
+            // both halves of a wave join; lanes 32 and up then hold the second 32
+            // rows (CX = 2), so that the store needs no branch, whose wait would
+            // hold up the loads of the tile to come (blkmax has room for a last
+            // tile's blocks beyond the items).  A wave's values follow one another.
+            const float v = max_halves(top[0], top[CX - 1]);
+            const int32_t row = (int32_t)x0 + (CX == 2 ? lane : lane & 31);
+            A.blkmax[((int64_t)(row >> 6) * A.nblk + (y >> 5)) * 64 + (row & 63)] = v;
+            group = fmaxf(group, v);
+        }
+    };
+    auto keep_group = [&](int64_t end) {  // after whole groups, and after the items
+        if constexpr (TOP) {
+            if (A.sup && ((end & ((32 << A.g_log) - 1)) == 0 || end >= A.F.count)) {
+                const int64_t row = x0 + (CX == 2 ? lane : lane & 31);
+                if (row < A.T) A.sup[row * A.ngrp + ((end - 1) >> (5 + A.g_log))] = group;
+                group = kOff;
+            }
         }
     };
     if (i0 < i1) {
@@ -341,68 +379,46 @@ __global__ __launch_bounds__(kThreads, 2) void k_score_pass(ScoreK A) {
         t.load(A.F, i0 + YT);
         put(1, i0 + YT);
         __syncthreads();
+        using Offsets = std::integral_constant<bool, BIAS>;
         f16 acc[CX];
-#pragma unroll
-        for (int q = 0; q < CX; ++q) acc[q] = scores<K, NP, YT>(buf(0), x[q]);
+        start(buf(0), 0, acc, Offsets());
         int cur = 0;
-        auto work = [&](int64_t y0, const uint16_t *b, const uint16_t *b_next, auto masked) {
-            const float *off = reinterpret_cast<const float *>(b + NP * TL::kPlane) + 4 * h;
+        int64_t y0 = i0;
+        for (; BIAS ? y0 < i1 : y0 + YT <= i1; y0 += YT) {
+            const int nxt = cur == 2 ? 0 : cur + 1, far = nxt == 2 ? 0 : nxt + 1;
+            t.load(A.F, y0 + 2 * YT);
 #pragma unroll
             for (int u = 0; u < YT / 32; ++u) {
-                const uint16_t *y = u + 1 < YT / 32 ? b + (u + 1) * 32 * S::RS : b_next;
                 f16 next[CX];
                 float top[CX];
-                if constexpr (masked()) {  // a tile now and then, or a biased table: one after the other, in fewer registers
+                start(u + 1 < YT / 32 ? buf(cur) : buf(nxt), u + 1 < YT / 32 ? u + 1 : 0, next, Offsets());
 #pragma unroll
-                    for (int q = 0; q < CX; ++q) top[q] = take<ENT, true>(st[q], acc[q], A.c, off + 32 * u);
-                    __builtin_amdgcn_sched_barrier(0);
+                for (int q = 0; q < CX; ++q) top[q] = take<ENT>(st[q], acc[q], A.c);
+                constexpr int kProducts = CX * S::KS * (NP == 1 ? 1 : 6), kVector = CX * (ENT ? 76 : 60);
+#pragma unroll
+                for (int g = 0; g < kProducts; ++g) {
+                    __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);  // a matrix product, then its share of vector work
+                    __builtin_amdgcn_sched_group_barrier(0x2, (kVector + kProducts - 1) / kProducts, 0);
                 }
-#pragma unroll
-                for (int q = 0; q < CX; ++q) next[q] = scores<K, NP, YT>(y, x[q]);
-                if constexpr (!masked()) {
-#pragma unroll
-                    for (int q = 0; q < CX; ++q) top[q] = take<ENT, false>(st[q], acc[q], A.c, nullptr);
-                    constexpr int kProducts = CX * S::KS * (NP == 1 ? 1 : 6), kVector = CX * (ENT ? 76 : 60);
-#pragma unroll
-                    for (int g = 0; g < kProducts; ++g) {
-                        __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);  // a matrix product, then its share of vector work
-                        __builtin_amdgcn_sched_group_barrier(0x2, (kVector + kProducts - 1) / kProducts, 0);
-                    }
-                }
-                if constexpr (TOP) {
-                    // both halves of a wave join; lanes 32 and up then hold the
-                    // second 32 rows (CX = 2), so that the store needs no branch,
-                    // whose wait would hold up the loads of the tile to come
-                    if (!masked() || y0 + 32 * u < i1) {
-                        const int64_t blk = (y0 >> 5) + u;
-                        const float v = max_halves(top[0], top[CX - 1]);
-                        const int32_t row = (int32_t)x0 + (CX == 2 ? lane : lane & 31);
-                        // (a wave's values follow one another in memory)
-                        A.blkmax[((int64_t)(row >> 6) * A.nblk + blk) * 64 + (row & 63)] = v;
-                        group = fmaxf(group, v);
-                    }
-                }
+                keep(top, y0 + 32 * u);
                 __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
                 for (int q = 0; q < CX; ++q) acc[q] = next[q];
             }
-        };
-        for (int64_t y0 = i0; y0 < i1; y0 += YT) {
-            const int nxt = cur == 2 ? 0 : cur + 1, far = nxt == 2 ? 0 : nxt + 1;
-            t.load(A.F, y0 + 2 * YT);
-            if (special(y0)) work(y0, buf(cur), buf(nxt), std::true_type());
-            else work(y0, buf(cur), buf(nxt), std::false_type());
-            if constexpr (TOP) {
-                const int64_t end = y0 + YT;  // of whole groups, or of the items
-                if (A.sup && ((end & ((32 << A.g_log) - 1)) == 0 || end >= A.F.count)) {
-                    const int64_t row = x0 + (CX == 2 ? lane : lane & 31);
-                    if (row < A.T) A.sup[row * A.ngrp + ((end - 1) >> (5 + A.g_log))] = group;
-                    group = kOff;
-                }
-            }
+            keep_group(y0 + YT);
             put(far, y0 + 2 * YT);
             __syncthreads();
             cur = nxt;
+        }
+        if (!BIAS && y0 < i1) {  // the items' last, partial tile
+            for (int u = 0; u < YT / 32; ++u) {
+                float top[CX];
+                start(buf(cur), u, acc, std::true_type());
+#pragma unroll
+                for (int q = 0; q < CX; ++q) top[q] = take<ENT>(st[q], acc[q], A.c);
+                keep(top, y0 + 32 * u);
+            }
+            keep_group(y0 + YT);
         }
     }
 #pragma unroll
@@ -432,34 +448,30 @@ __global__ __launch_bounds__(kThreads, 2) void k_score_few(ScoreK A) {
     const int64_t w0 = i0 + wave * (A.slice_items / 4), w1 = std::min<int64_t>(w0 + A.slice_items / 4, i1);
     for (int64_t y0 = w0; y0 < w1; y0 += 32) {
         const int64_t item = y0 + (lane & 31);
-        float o = kOff;
+        float o = A.off;
         if (item < i1) {
             o = A.F.bias ? A.F.bias[item] : 0.f;
-            o = o < kExcluded ? kOff : o * A.bias_c;
+            o = o < kExcluded ? A.off : o * A.bias_c;
         }
         Raw<NP> raw[S::KS];
 #pragma unroll
         for (int s = 0; s < S::KS; ++s) {
             const int c = 16 * s + 8 * h;
             raw[s] = zero_raw<NP>();
-            if (o != kOff && c < K) raw[s] = load_raw<NP>(A.F.p, item * A.F.ld + c);
+            if (o != A.off && c < K) raw[s] = load_raw<NP>(A.F.p, item * A.F.ld + c);
         }
         f16 acc = {};
+        if (A.F.bias || y0 + 32 > i1) {
+#pragma unroll
+            for (int r = 0; r < 16; ++r) acc[r] = __shfl(o, tile_row(r) + 4 * h, 64);
+        }
 #pragma unroll
         for (int s = 0; s < S::KS; ++s) {
             b8 a[NP];
             parts_of<NP>(raw[s], a);
             acc = product<NP>(a, x[s], acc);
         }
-        float top;
-        if (A.F.bias || y0 + 32 > i1) {
-            __align__(16) float off[32];  // offsets of rows 4 h + 8 q + j at 8 q + j
-#pragma unroll
-            for (int r = 0; r < 16; ++r) off[tile_row(r)] = __shfl(o, tile_row(r) + 4 * h, 64);
-            top = take<ENT, true>(st, acc, A.c, off);
-        } else {
-            top = take<ENT, false>(st, acc, A.c, nullptr);
-        }
+        const float top = take<ENT>(st, acc, A.c);
         if (A.blkmax) {
             const int64_t blk = y0 >> 5;
             const float v = max_halves(top, top);
@@ -567,7 +579,7 @@ struct FinishK {
     float *loss;
     int32_t top;
     const float *blkmax, *sup;
-    int64_t nblk, ngrp;
+    int64_t blocks, nblk, ngrp;  // blocks of items; room for them in a row of blkmax
     int32_t g_log, width;  // rows that lie together in blkmax
     int32_t *top_ids;
     float *top_logp;
@@ -734,11 +746,11 @@ __global__ __launch_bounds__(kThreads) void k_score_finish(FinishK A) {
             });
             got = choose((int64_t)groups << A.g_log, want, pick[1], [&](int64_t j, float &v, int32_t &p) {
                 const int64_t b = ((int64_t)pick[0][j >> A.g_log] << A.g_log) + (j & ((1 << A.g_log) - 1));
-                v = b < A.nblk ? maxima[b * A.width] : -INFINITY;
+                v = b < A.blocks ? maxima[b * A.width] : -INFINITY;
                 p = (int32_t)b;
             });
         } else {
-            got = choose(A.nblk, want, pick[1], [&](int64_t j, float &v, int32_t &p) {
+            got = choose(A.blocks, want, pick[1], [&](int64_t j, float &v, int32_t &p) {
                 v = maxima[j * A.width];
                 p = (int32_t)j;
             });
@@ -854,6 +866,7 @@ struct GradK {
     float c;
     int turn;
     float bias_c;
+    float unit;        // of the offsets per row of Y: 1 / c where the scores start from them (bf16), else 1
     const float4 *coef;
     int64_t slice_rows;
     int32_t n_slices, n_tiles;
@@ -880,7 +893,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_grad_pass(GradK A) {
     const int64_t i0 = slice * A.slice_rows, i1 = std::min<int64_t>(i0 + A.slice_rows, A.Y.count);
     auto buf = [&](int b) { return reinterpret_cast<uint16_t *>(smem + b * TL::kBytes); };
     if constexpr (K < 32) {
-        for (size_t j = threadIdx.x; j < 2 * TL::kBytes / 4; j += kThreads) reinterpret_cast<uint32_t *>(smem)[j] = 0u;
+        for (size_t j = threadIdx.x; j < 3 * TL::kBytes / 4; j += kThreads) reinterpret_cast<uint32_t *>(smem)[j] = 0u;
         __syncthreads();
     }
     b8 x[S::KS][NP];
@@ -904,11 +917,11 @@ __global__ __launch_bounds__(kThreads, 2) void k_grad_pass(GradK A) {
         t.store(A.Y, y0, (!ITEMS && A.Y.bias) || y0 + YT > A.Y.count, b);
         if (threadIdx.x < YT) {
             const int64_t i = y0 + threadIdx.x;
-            float *o = reinterpret_cast<float *>(b + NP * TL::kPlane) + threadIdx.x;
+            float *o = reinterpret_cast<float *>(b + NP * TL::kPlane) + offset_place(threadIdx.x);
             if constexpr (ITEMS) {
                 float4 q = make_float4(-kLeast, 0.f, 0.f, 0.f);
                 if (i < i1) q = A.coef[i];
-                o[0] = -q.x;
+                o[0] = -q.x * A.unit;
                 o[YT] = q.y;
                 o[2 * YT] = q.z;
             } else {
@@ -917,77 +930,97 @@ __global__ __launch_bounds__(kThreads, 2) void k_grad_pass(GradK A) {
                     v = A.Y.bias ? A.Y.bias[i] : 0.f;
                     v = v < kExcluded ? kOff : v * A.bias_c;
                 }
-                o[0] = v;
+                o[0] = v * A.unit;
             }
         }
     };
     const int grp = lane >> 4, gi = lane & 15;
-    int cur = 0;
-    if (i0 < i1) {  // nothing to read of an empty side
-        t.load(A.Y, i0);
-        put(buf(0), i0);
-    }
-    __syncthreads();
-    for (int64_t y0 = i0; y0 < i1; y0 += YT) {
-        const bool more = y0 + YT < i1;
-        if (more) t.load(A.Y, y0 + YT);
-        const uint16_t *b = buf(cur);
+    auto offsets = [&](const uint16_t *b, int u) {
+        return reinterpret_cast<const float *>(b + NP * TL::kPlane) + 32 * u + 4 * h;
+    };
+    // the scores of block u of a tile; bf16: from the offsets.  fp32: those are
+    // added to the exponents, so that no sum is rounded at their size.
+    auto start = [&](const uint16_t *b, int u) {
+        return scores<K, NP, YT>(b + u * 32 * S::RS, x, NP == 1 ? per_row(offsets(b, u)) : f16{});
+    };
+    // ... their g, in the parts that the second product takes
+    auto weights = [&](const f16 &s, const float *off, b8 (&ga)[2][NP]) {
 #pragma unroll
-        for (int u = 0; u < YT / 32; ++u) {
-            const uint16_t *yt = b + u * 32 * S::RS;
-            const float *off = reinterpret_cast<const float *>(b + NP * TL::kPlane) + 32 * u + 4 * h;
-            f16 g = scores<K, NP, YT>(yt, x);
+        for (int h2 = 0; h2 < 2; ++h2) {
+            f8 g;
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const f4 o = *reinterpret_cast<const f4 *>(off + 8 * q);
-                f4 ya = {}, yb = {};
+            for (int q = 2 * h2; q < 2 * h2 + 2; ++q) {
+                f4 o = {}, ya = {}, yb = {};
+                if constexpr (NP != 1) o = *reinterpret_cast<const f4 *>(off + 8 * q);
                 if constexpr (ITEMS) {
                     ya = *reinterpret_cast<const f4 *>(off + YT + 8 * q);
                     if constexpr (ENT) yb = *reinterpret_cast<const f4 *>(off + 2 * YT + 8 * q);
                 }
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    const float e = fmaf(g[4 * q + j], A.c, o[j] + own_off);
+                    const float e = fmaf(s[4 * q + j], A.c, NP == 1 ? own_off : o[j] + own_off);
                     const float p = __builtin_amdgcn_exp2f(e);
-                    if constexpr (ITEMS) g[4 * q + j] = p * (ENT ? fmaf(e, yb[j], ya[j]) : ya[j]);
-                    else g[4 * q + j] = ENT ? p * fmaf(e, own_b, own_a) : p;
+                    if constexpr (ITEMS) g[4 * (q & 1) + j] = p * (ENT ? fmaf(e, yb[j], ya[j]) : ya[j]);
+                    else g[4 * (q & 1) + j] = ENT ? p * fmaf(e, own_b, own_a) : p;
                 }
             }
+            if constexpr (NP == 1) ga[h2][0] = __builtin_convertvector(g, b8);
+            else split3(g, ga[h2]);
+        }
+    };
+    // acc += g times the 32 rows at yt
+    auto products = [&](const uint16_t *yt, const b8 (&ga)[2][NP]) {
 #pragma unroll
-            for (int s = 0; s < 2; ++s) {
-                const f8 gs = {g[8 * s], g[8 * s + 1], g[8 * s + 2], g[8 * s + 3],
-                               g[8 * s + 4], g[8 * s + 5], g[8 * s + 6], g[8 * s + 7]};
-                b8 ga[NP];
-                if constexpr (NP == 1) ga[0] = __builtin_convertvector(gs, b8);
-                else split3(gs, ga);
+        for (int h2 = 0; h2 < 2; ++h2) {
 #pragma unroll
-                for (int nb = 0; nb < S::NB; ++nb) {
-                    // in each group of 16 lanes, lane i receives element i % 4
-                    // of the 8-byte pieces of lanes i / 4, 4 + i / 4, ...: lane
-                    // 4 j + q points at row j, coordinates 4 q .. 4 q + 3
-                    const uint16_t *src = yt + (16 * s + 4 * h + (gi >> 2)) * S::RS + nb * 32 + (grp & 1) * 16 + 4 * (gi & 3);
-                    b8 yb[NP];
+            for (int nb = 0; nb < S::NB; ++nb) {
+                // in each group of 16 lanes, lane i receives element i % 4 of
+                // the 8-byte pieces of lanes i / 4, 4 + i / 4, ...: lane 4 j + q
+                // points at row j, coordinates 4 q .. 4 q + 3 (the two groups of a
+                // half wave half a row apart, 32 banks at k = 128)
+                const uint16_t *src = yt + (16 * h2 + 2 * (gi >> 2) + h) * S::RS + nb * 16 + (grp & 1) * (S::KW / 2) + 4 * (gi & 3);
+                b8 yb[NP];
 #pragma unroll
-                    for (int p = 0; p < NP; ++p) {
-                        const uint16_t *at = src + p * TL::kPlane;
-                        const uint2 lo = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                                                                       (__attribute__((address_space(3))) s4 *)(at)));
-                        const uint2 hi = __builtin_bit_cast(
-                            uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                                       (__attribute__((address_space(3))) s4 *)(at + 8 * S::RS)));
-                        yb[p] = __builtin_bit_cast(b8, make_uint4(lo.x, lo.y, hi.x, hi.y));
-                    }
-                    acc[nb] = product<NP>(ga, yb, acc[nb]);
+                for (int p = 0; p < NP; ++p) {
+                    const uint16_t *at = src + p * TL::kPlane;
+                    const uint2 lo = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                                                                   (__attribute__((address_space(3))) s4 *)(at)));
+                    const uint2 hi = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                                                                   (__attribute__((address_space(3))) s4 *)(at + 8 * S::RS)));
+                    yb[p] = __builtin_bit_cast(b8, make_uint4(lo.x, lo.y, hi.x, hi.y));
                 }
+                acc[nb] = product<NP>(ga[h2], yb, acc[nb]);
             }
         }
-        if (more) put(buf(cur ^ 1), y0 + YT);
+    };
+    if (i0 < i1) {  // nothing to read of an empty side
+        t.load(A.Y, i0);
+        put(buf(0), i0);
+        t.load(A.Y, i0 + YT);
+        put(buf(1), i0 + YT);
         __syncthreads();
-        cur ^= 1;
+        f16 s = start(buf(0), 0);
+        int cur = 0;
+        for (int64_t y0 = i0; y0 < i1; y0 += YT) {
+            const int nxt = cur == 2 ? 0 : cur + 1, far = nxt == 2 ? 0 : nxt + 1;
+            t.load(A.Y, y0 + 2 * YT);
+#pragma unroll
+            for (int u = 0; u < YT / 32; ++u) {
+                b8 ga[2][NP];
+                const f16 next = start(u + 1 < YT / 32 ? buf(cur) : buf(nxt), u + 1 < YT / 32 ? u + 1 : 0);
+                weights(s, offsets(buf(cur), u), ga);
+                products(buf(cur) + u * 32 * S::RS, ga);
+                __builtin_amdgcn_sched_barrier(0);  // else reads of many blocks ahead spill
+                s = next;
+            }
+            put(buf(far), y0 + 2 * YT);
+            __syncthreads();
+            cur = nxt;
+        }
     }
 #pragma unroll
     for (int nb = 0; nb < S::NB; ++nb) {
-        const int c = nb * 32 + (lane & 31);
+        const int c = nb * 16 + (grp & 1) * (S::KW / 2) + gi;
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
             const int64_t row = x0 + tile_row(r) + 4 * h;
@@ -1033,16 +1066,27 @@ __global__ __launch_bounds__(kThreads) void k_grad_rows(const float *part, int32
 
 constexpr int kCus = 256;
 
-// Slices of a streamed side: about `wanted` workgroups in all, slices of at
-// least `least` rows and whole tiles; a multiple of the 8 XCDs from 8 on.
-void slices_of(int64_t rows, int64_t tiles, int64_t wanted, int64_t least, int64_t unit, int32_t &n_slices,
-               int64_t &slice_rows) {
-    int64_t ns = std::max<int64_t>(1, (wanted + tiles - 1) / std::max<int64_t>(tiles, 1));
-    ns = std::min<int64_t>(ns, std::max<int64_t>(1, rows / least));
-    if (ns >= 8) ns = ns / 8 * 8;
-    slice_rows = ((rows + ns - 1) / ns + unit - 1) / unit * unit;
-    slice_rows = std::max<int64_t>(slice_rows, unit);
-    n_slices = (int32_t)std::max<int64_t>(1, (rows + slice_rows - 1) / slice_rows);
+// How a streamed side of `rows` rows is cut: `tiles` workgroups per slice, of
+// which two fit a CU; slices of whole units, a multiple of the 8 XCDs from 8
+// on.  Chosen by the time it takes: rounds of workgroups, each its slice and a
+// start that takes as long as about 96 rows, and `slice_cost`, what a
+// slice's sums cost to write and add, in rows.
+void slices_of(int64_t rows, int64_t tiles, int64_t unit, double slice_cost, int32_t &n_slices, int64_t &slice_rows) {
+    double best = 0.0;
+    n_slices = 1;
+    slice_rows = unit;
+    for (int64_t ns = 1; ns <= 2048; ns += ns < 8 ? 1 : 8) {
+        const int64_t each = std::max<int64_t>(unit, ((rows + ns - 1) / ns + unit - 1) / unit * unit);
+        const int64_t used = std::max<int64_t>(1, (rows + each - 1) / each);
+        const double rounds = (double)((used * tiles + 2 * kCus - 1) / (2 * kCus));
+        const double cost = rounds * ((double)each + 96.0) + (double)used * slice_cost;
+        if (ns == 1 || cost < best) {
+            best = cost;
+            n_slices = (int32_t)used;
+            slice_rows = each;
+        }
+        if (each == unit) break;
+    }
 }
 
 struct ScorePlan {
@@ -1058,7 +1102,7 @@ struct ScorePlan {
 
 ScorePlan plan_score(int64_t T, int64_t n, int prec, int top, Carve &c) {
     ScorePlan p{};
-    p.nblk = (n + 31) / 32;
+    p.nblk = (n + 63) / 64 * 2;
     p.few = T <= 32;
     p.chunk = T;
     if (top > 0) {  // at most 1 GiB of block maxima at a time
@@ -1073,12 +1117,12 @@ ScorePlan plan_score(int64_t T, int64_t n, int prec, int top, Carve &c) {
     p.padded = T;
     if (p.few) {
         p.n_tiles = 1;
-        slices_of(n, 1, 2 * kCus, 128, 128 * G, p.n_slices, p.slice_items);
+        slices_of(n, 1, 128 * G, 0.0, p.n_slices, p.slice_items);
     } else {
         const int64_t rows = 128 * p.cx;
         p.n_tiles = (int32_t)((p.chunk + rows - 1) / rows);
         p.padded = p.n_tiles * rows;
-        slices_of(n, p.n_tiles, 4 * kCus, 256, std::max<int64_t>(64, 32 * G), p.n_slices, p.slice_items);
+        slices_of(n, p.n_tiles, std::max<int64_t>(64, 32 * G), 0.5, p.n_slices, p.slice_items);
     }
     p.part = c.take<float4>((int64_t)p.n_slices * p.chunk);
     if (top > 0) {
@@ -1102,11 +1146,11 @@ void allow_lds(const void *kernel, size_t lds, std::atomic<uint64_t> &done) {
 // (2,048 x 1 M, k = 128: 555 us; 32 rows: 647 us).  Tiles of 64 rows of F, but of
 // 32 where the blocks' maxima are kept, whose registers would spill otherwise
 // (880 and 992 us with the best 20).  fp32: 32 rows and tiles of 32, three parts each.
-template <int K, int NP, bool ENT, bool TOP>
+template <int K, int NP, bool BIAS, bool ENT, bool TOP>
 void launch_score_pass(const ScoreK &a, hipStream_t s) {
-    constexpr int CX = NP == 1 ? 2 : 1, YT = NP == 1 && !TOP ? 64 : 32;
+    constexpr int CX = NP == 1 ? 2 : 1, YT = NP == 1 ? 64 : 32;
     constexpr size_t lds = 3 * Tile<K, NP, YT>::kBytes;
-    auto *pass = &k_score_pass<K, NP, CX, YT, ENT, TOP>;
+    auto *pass = &k_score_pass<K, NP, CX, YT, BIAS, ENT, TOP>;
     if (lds > 64 * 1024) {  // more dynamic LDS than the default limit: said once per kernel and device
         static std::atomic<uint64_t> done;
         allow_lds(reinterpret_cast<const void *>(pass), lds, done);
@@ -1119,26 +1163,35 @@ void launch_score(const ScoreK &a, const ScorePlan &p, hipStream_t s) {
     if (p.few) {
         k_score_few<K, NP, ENT><<<p.n_slices, kThreads, 0, s>>>(a);
     } else {
-        if (a.blkmax) launch_score_pass<K, NP, ENT, true>(a, s);
-        else launch_score_pass<K, NP, ENT, false>(a, s);
+        const bool bias = a.F.bias != nullptr;
+        if (a.blkmax) bias ? launch_score_pass<K, NP, true, ENT, true>(a, s) : launch_score_pass<K, NP, false, ENT, true>(a, s);
+        else bias ? launch_score_pass<K, NP, true, ENT, false>(a, s) : launch_score_pass<K, NP, false, ENT, false>(a, s);
     }
+    TSID_HIP(hipGetLastError());
+}
+
+template <int K, int NP, bool ITEMS, bool ENT>
+void launch_grad_pass(const GradK &a, hipStream_t s) {
+    constexpr int YT = NP == 1 ? 64 : 32;
+    constexpr size_t lds = 3 * Tile<K, NP, YT>::kBytes;
+    auto *pass = &k_grad_pass<K, NP, YT, ITEMS, ENT>;
+    if (lds > 64 * 1024) {
+        static std::atomic<uint64_t> done;
+        allow_lds(reinterpret_cast<const void *>(pass), lds, done);
+    }
+    pass<<<grid_of(a.n_slices, a.n_tiles), kThreads, lds, s>>>(a);
     TSID_HIP(hipGetLastError());
 }
 
 template <int K, int NP>
 void launch_grad(bool items, bool ent, const GradK &a, hipStream_t s) {
-    constexpr int YT = NP == 1 ? 64 : 32;
-    constexpr size_t lds = 2 * Tile<K, NP, YT>::kBytes;
-    static_assert(lds <= 64 * 1024, "within the default limit of dynamic LDS");
-    const int grid = grid_of(a.n_slices, a.n_tiles);
     if (items) {
-        if (ent) k_grad_pass<K, NP, YT, true, true><<<grid, kThreads, lds, s>>>(a);
-        else k_grad_pass<K, NP, YT, true, false><<<grid, kThreads, lds, s>>>(a);
+        if (ent) launch_grad_pass<K, NP, true, true>(a, s);
+        else launch_grad_pass<K, NP, true, false>(a, s);
     } else {
-        if (ent) k_grad_pass<K, NP, YT, false, true><<<grid, kThreads, lds, s>>>(a);
-        else k_grad_pass<K, NP, YT, false, false><<<grid, kThreads, lds, s>>>(a);
+        if (ent) launch_grad_pass<K, NP, false, true>(a, s);
+        else launch_grad_pass<K, NP, false, false>(a, s);
     }
-    TSID_HIP(hipGetLastError());
 }
 
 // f.template operator()<K, NP>() for the rank and precision at hand.
@@ -1160,14 +1213,20 @@ void for_rank(int k, int prec, Fn &&f) {
 
 Side side_of(const Rows &r, const float *bias) { return Side{r.p, r.count, r.ld, bias}; }
 
+// c and the sign of the scores; scale 0 is X = 0 and c = 1.
+void exponent_of(const Head &h, float &c, int &turn) {
+    c = h.scale == 0.f ? 1.f : (float)(std::fabs((double)h.scale) * kLog2e);
+    turn = h.scale == 0.f ? kNone : h.scale < 0.f ? kTurn : kKeep;
+}
+
 // The pass over all items and the rows' results, a run of rows at a time.
 void score_rows(const Head &h, const ScorePlan &p, FinishK f, bool entropy, hipStream_t s) {
     ScoreK a{};
     a.H = side_of(h.H, nullptr);
     a.F = side_of(h.F, h.bias);
-    a.c = (float)(std::fabs((double)h.scale) * kLog2e);
-    a.turn = h.scale < 0.f;
-    a.bias_c = (float)((double)h.bias_scale * kLog2e);
+    exponent_of(h, a.c, a.turn);
+    a.bias_c = (float)((double)h.bias_scale * kLog2e / (double)a.c);
+    a.off = kOff / a.c;
     a.slice_items = p.slice_items;
     a.n_slices = p.n_slices;
     a.part = p.part;
@@ -1185,6 +1244,7 @@ void score_rows(const Head &h, const ScorePlan &p, FinishK f, bool entropy, hipS
     f.bias_scale = h.bias_scale;
     f.blkmax = p.blkmax;
     f.sup = p.sup;
+    f.blocks = (h.F.count + 31) / 32;
     f.nblk = p.nblk;
     f.ngrp = p.ngrp;
     for (int64_t t0 = 0; t0 < h.H.count; t0 += p.chunk) {
@@ -1212,17 +1272,20 @@ struct GradPlan {
     SumPlan sum;
 };
 
-GradPlan plan_grad(int64_t T, int64_t n, int k, int per_row, Carve &c) {
+GradPlan plan_grad(int64_t T, int64_t n, int k, int prec, int n_ids, Carve &c) {
     GradPlan p{};
     p.h_tiles = (int32_t)((T + 127) / 128);
     p.f_tiles = (int32_t)((n + 127) / 128);
-    slices_of(n, p.h_tiles, 4 * kCus, 256, 64, p.h_slices, p.h_rows);
-    slices_of(T, p.f_tiles, 4 * kCus, 256, 64, p.f_slices, p.f_rows);
+    // a slice's part of the sums, 8 k bytes a row of X written and read, at 4
+    // bytes a ns, against 30 ns a streamed row (128 ns in fp32) for a workgroup
+    const double per_row = 2e-3 * k / (prec == TSID_BF16 ? 30.0 : 128.0);
+    slices_of(n, p.h_tiles, 64, per_row * (double)T, p.h_slices, p.h_rows);
+    slices_of(T, p.f_tiles, 64, per_row * (double)n, p.f_slices, p.f_rows);
     p.coef = c.take<float4>(T);
-    p.w = c.take<float>(T * per_row);
+    p.w = c.take<float>(T * n_ids);
     // the two sides take turns at the same parts
     p.part = c.take<float>(std::max<int64_t>((int64_t)p.h_slices * T, (int64_t)p.f_slices * n) * k);
-    p.sum.entries = T * per_row;
+    p.sum.entries = T * n_ids;
     p.sum.n = n;
     p.sum.k = k;
     carve_sum(p.sum, c);
@@ -1271,22 +1334,22 @@ void run_distill(const Head &h, const DistillOut &o, void *ws, int32_t *err, hip
 
 size_t head_grad_workspace(int64_t T, int64_t n, int k, int prec, int per_row) {
     Carve c;
-    plan_grad(T, n, k, per_row, c);
+    plan_grad(T, n, k, prec, per_row, c);
     return c.used;
 }
 
 void run_head_grad(const Head &h, const HeadGrad &g, void *ws, int32_t *err, hipStream_t s) {
     const int64_t T = h.H.count, n = h.F.count;
     Carve c{static_cast<char *>(ws)};
-    GradPlan p = plan_grad(T, n, h.k, g.per_row, c);
+    GradPlan p = plan_grad(T, n, h.k, h.prec, g.per_row, c);
     const bool ent = g.dentropy != nullptr;
     if (T > 0) {
         k_head_coef<<<ceil_div(T, 4), kThreads, 0, s>>>(g, T, n, h.bias, p.coef, p.w, err);
         TSID_HIP(hipGetLastError());
     }
     GradK a{};
-    a.c = (float)(std::fabs((double)h.scale) * kLog2e);
-    a.turn = h.scale < 0.f;
+    exponent_of(h, a.c, a.turn);
+    a.unit = h.prec == TSID_BF16 ? 1.f / a.c : 1.f;
     a.bias_c = (float)((double)h.bias_scale * kLog2e);
     a.coef = p.coef;
     a.part = p.part;

@@ -79,7 +79,7 @@ struct Head {
     float bias_scale;  // 1 / temperature
 };
 // A bias below this excludes its item: its row of F is never used.
-constexpr float kExcluded = -1e20f;
+constexpr float kExcluded = -1e7f;
 
 struct ScoreOut {
     const int32_t *ids;

@@ -5,7 +5,7 @@ sums of absolute values; nothing in it comes from a run."""
 import numpy as np
 
 U, V = 2.0 ** -24, 2.0 ** -8
-EXCLUDED = -1e20
+EXCLUDED = -1e7
 
 
 def softmax_over(H, F, scale, bias, tau):

@@ -141,7 +141,7 @@ def _problem(seed, T, n, k, prec, bias, m, ld=0):
     if bias is not None:
         b = g.normal(0, 1, n).astype(np.float32)
         out = g.random(n) < (0.2 if bias == "some" else 2.0)
-        b[out] = g.choice(np.array([-np.inf, np.finfo(np.float32).min, -1.1e20], np.float32), int(out.sum()))
+        b[out] = g.choice(np.array([-np.inf, np.finfo(np.float32).min, -1.1e7], np.float32), int(out.sum()))
         F[torch.from_numpy(out).cuda()] = _gpu(g.choice(np.array([np.nan, np.inf, -np.inf, 1e30], np.float32),
                                                         (int(out.sum()), k))).to(F.dtype)
         Fd[out] = 0.0
@@ -524,7 +524,7 @@ def test_refusals(X):
     _refused(1, X.score, H, F, ids=i(4, 2).long())
     _refused(1, X.score, H, F, top=65)
     _refused(1, X.score, H, F, top=-1)
-    for s in (float("nan"), float("inf"), 1e39):
+    for s in (float("nan"), float("inf"), 1e39, 1e13, 1e-13):
         _refused(1, X.score, H, F, scale=s)
     te, lse = z(4, 2), z(4)
     for tau in (0.0, -1.0, 1e-7, 1e7, float("nan")):
