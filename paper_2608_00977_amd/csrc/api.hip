@@ -3088,8 +3088,9 @@ tsid_status tsid_lookup_grad(tsid_ctx *c, int32_t prec, int32_t k, const tsid_ro
         Carve carve{static_cast<char *>(ws)};
         carve_sum(p, carve);
         hipStream_t s = static_cast<hipStream_t>(hip_stream);
-        launch_sum_sort(p, ids, nullptr, c->rows_err, s);
         SumArgs a{};
+        a.ids = ids;
+        a.err = c->rows_err;
         a.X = g;
         a.per_row = 1;
         a.scale = scale;

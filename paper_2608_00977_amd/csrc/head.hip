@@ -1029,36 +1029,40 @@ __global__ __launch_bounds__(kThreads, 2) void k_grad_pass(GradK A) {
     }
 }
 
-__device__ __forceinline__ float factor(float v) { return v; }
-__device__ __forceinline__ float factor(uint16_t v) { return __uint_as_float((uint32_t)v << 16); }
-
-// out[t] = scale (a_t * sum of the parts + sum_j w_tj F[id_tj]) (a_t in the parts already: coef null).
-template <typename E>
-__global__ __launch_bounds__(kThreads) void k_grad_rows(const float *part, int32_t n_parts, int64_t T, int k,
+// out[t] = scale (a_t * sum of the parts + sum_j w_tj F[id_tj]) (a_t in the
+// parts already: coef null); K / 8 lanes a row, four listed items in flight.
+template <typename E, int K>
+__global__ __launch_bounds__(kThreads) void k_grad_rows(const float *part, int32_t n_parts, int64_t T,
                                                         const float4 *coef, const int32_t *ids, const float *w,
                                                         int32_t per_row, const E *F, int64_t ldf, float scale, E *out,
                                                         int64_t ldo) {
-    const int64_t j = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-    const int64_t t = j / (k / 4);
-    const int c = (int)(j % (k / 4)) * 4;
+    constexpr int LN = K / 8, U = 4;
+    const int64_t t = ((int64_t)blockIdx.x * kThreads + threadIdx.x) / LN;
+    const int c = (int)(threadIdx.x % LN) * 8;
     if (t >= T) return;
-    f4 sum = {};
-    for (int32_t p = 0; p < n_parts; ++p) sum += *reinterpret_cast<const f4 *>(part + ((int64_t)p * T + t) * k + c);
+    f8 sum = {}, more = {};
+#pragma unroll 4
+    for (int32_t p = 0; p < n_parts; ++p) sum += load8(part + ((int64_t)p * T + t) * K + c);
     if (coef) sum *= coef[t].y;
-    f4 more = {};
-    for (int32_t q = 0; q < per_row; ++q) {
-        const float v = w[t * per_row + q];
-        if (v == 0.f) continue;  // also the entries that are no item's
-        const E *f = F + (int64_t)ids[t * per_row + q] * ldf + c;
+    for (int32_t q = 0; q < per_row; q += U) {
+        float v[U];
+        f8 f[U];
 #pragma unroll
-        for (int x = 0; x < 4; ++x) more[x] = fmaf(v, factor(f[x]), more[x]);
+        for (int u = 0; u < U; ++u) v[u] = q + u < per_row ? w[t * per_row + q + u] : 0.f;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            f[u] = f8{};
+            if (v[u] != 0.f) f[u] = load8(F + (int64_t)ids[t * per_row + q + u] * ldf + c);  // 0: also no item's entry
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) more += v[u] * f[u];
     }
     sum = (sum + more) * scale;
     if constexpr (sizeof(E) == 4) {
-        *reinterpret_cast<f4 *>(out + t * ldo + c) = sum;
+        *reinterpret_cast<f4 *>(out + t * ldo + c) = f4{sum[0], sum[1], sum[2], sum[3]};
+        *reinterpret_cast<f4 *>(out + t * ldo + c + 4) = f4{sum[4], sum[5], sum[6], sum[7]};
     } else {
-        typedef __bf16 b4 __attribute__((ext_vector_type(4)));
-        *reinterpret_cast<uint2 *>(out + t * ldo + c) = __builtin_bit_cast(uint2, __builtin_convertvector(sum, b4));
+        *reinterpret_cast<uint4 *>(out + t * ldo + c) = __builtin_bit_cast(uint4, __builtin_convertvector(sum, b8));
     }
 }
 
@@ -1069,7 +1073,7 @@ constexpr int kCus = 256;
 // How a streamed side of `rows` rows is cut: `tiles` workgroups per slice, of
 // which two fit a CU; slices of whole units, a multiple of the 8 XCDs from 8
 // on.  Chosen by the time it takes: rounds of workgroups, each its slice and a
-// start that takes as long as about 96 rows, and `slice_cost`, what a
+// start that takes as long as about 96 rows, the last round's uneven end, and `slice_cost`, what a
 // slice's sums cost to write and add, in rows.
 void slices_of(int64_t rows, int64_t tiles, int64_t unit, double slice_cost, int32_t &n_slices, int64_t &slice_rows) {
     double best = 0.0;
@@ -1079,7 +1083,7 @@ void slices_of(int64_t rows, int64_t tiles, int64_t unit, double slice_cost, int
         const int64_t each = std::max<int64_t>(unit, ((rows + ns - 1) / ns + unit - 1) / unit * unit);
         const int64_t used = std::max<int64_t>(1, (rows + each - 1) / each);
         const double rounds = (double)((used * tiles + 2 * kCus - 1) / (2 * kCus));
-        const double cost = rounds * ((double)each + 96.0) + (double)used * slice_cost;
+        const double cost = (rounds + 0.3) * ((double)each + 96.0) + (double)used * slice_cost;
         if (ns == 1 || cost < best) {
             best = cost;
             n_slices = (int32_t)used;
@@ -1360,16 +1364,13 @@ void run_head_grad(const Head &h, const HeadGrad &g, void *ws, int32_t *err, hip
         a.n_slices = p.h_slices;
         a.n_tiles = p.h_tiles;
         for_rank(h.k, h.prec, [&](auto kk, auto np) { launch_grad<kk(), np()>(false, ent, a, s); });
-        const int blocks = ceil_div(T * (h.k / 4), kThreads);
         const float4 *coef = ent ? nullptr : p.coef;
-        if (h.prec == TSID_BF16)
-            k_grad_rows<uint16_t><<<blocks, kThreads, 0, s>>>(p.part, p.h_slices, T, h.k, coef, g.ids, p.w, g.per_row,
-                                                              static_cast<const uint16_t *>(h.F.p), h.F.ld, h.scale,
-                                                              static_cast<uint16_t *>(g.dH.p), g.dH.ld);
-        else
-            k_grad_rows<float><<<blocks, kThreads, 0, s>>>(p.part, p.h_slices, T, h.k, coef, g.ids, p.w, g.per_row,
-                                                           static_cast<const float *>(h.F.p), h.F.ld, h.scale,
-                                                           static_cast<float *>(g.dH.p), g.dH.ld);
+        for_rank(h.k, h.prec, [&](auto kk, auto np) {
+            using E = std::conditional_t<np() == 1, uint16_t, float>;
+            k_grad_rows<E, kk()><<<ceil_div(T * (kk() / 8), kThreads), kThreads, 0, s>>>(
+                p.part, p.h_slices, T, coef, g.ids, p.w, g.per_row, static_cast<const E *>(h.F.p), h.F.ld, h.scale,
+                static_cast<E *>(g.dH.p), g.dH.ld);
+        });
         TSID_HIP(hipGetLastError());
     }
     if (g.dF.p && n > 0) {
@@ -1381,8 +1382,10 @@ void run_head_grad(const Head &h, const HeadGrad &g, void *ws, int32_t *err, hip
             a.n_tiles = p.f_tiles;
             for_rank(h.k, h.prec, [&](auto kk, auto np) { launch_grad<kk(), np()>(true, ent, a, s); });
         }
-        launch_sum_sort(p.sum, g.ids, h.bias, err, s);
         SumArgs sa{};
+        sa.ids = g.ids;
+        sa.bias = h.bias;
+        sa.err = err;
         sa.X = h.H;
         sa.w = p.w;
         sa.per_row = std::max(1, g.per_row);

@@ -45,18 +45,24 @@ struct SumPlan {
     uint32_t *ptr;       // n + 1: first sorted entry of each row
     float *carry[2];     // sums of pieces of long rows, two per piece (two levels)
     bool alt;            // where the sort left its result
+    bool scan;           // few entries: no sort, none of these pieces
 };
 // Entries one piece of a long row's sum takes, and the row length from which
 // a row is summed in pieces.
 constexpr int kSumPiece = 64;
+// Entries, and comparisons of ids, up to which every row looks through all
+// ids: the sort and what follows it cost six launches and about 35 us, the
+// scan one launch and about 10 us at these bounds.
+constexpr int64_t kScanEntries = 2048, kScanCompares = int64_t(1) << 27;
 void carve_sum(SumPlan &p, Carve &c);
-// Sorts the entries by id (entries whose id is not in [0, n), or whose row of
-// the table is excluded by bias, go last and add nothing; ids other than -1
-// outside the table set ERR_RANGE).
-void launch_sum_sort(SumPlan &p, const int32_t *ids, const float *bias, int32_t *err, hipStream_t s);
 // out[i] = scale * (sum of the entries of i + sum of the parts' rows i), every
 // row of out written; parts: n_parts fp32 arrays of n x k, part_stride apart.
+// An entry whose id is -1, or whose row of the table is excluded by bias, adds
+// nothing; one with another id outside the table neither, and sets ERR_RANGE.
 struct SumArgs {
+    const int32_t *ids;
+    const float *bias;
+    int32_t *err;
     Rows X;
     const float *w;
     int32_t per_row;
@@ -66,7 +72,7 @@ struct SumArgs {
     float scale;
     Rows out;
 };
-void launch_sum_rows(const SumPlan &p, int prec, const SumArgs &a, hipStream_t s);
+void launch_sum_rows(SumPlan &p, int prec, const SumArgs &a, hipStream_t s);
 
 // ------------------------------------------------------------------- head
 // Scores z_ti = scale h_t . f_i + bias_i of all items for all rows, divided by

@@ -119,36 +119,53 @@ struct SumK {
     int64_t ldo;
 };
 
-// Sum of the sorted entries e0 .. e1 - 1 in order, four rows in flight.
-template <typename E>
+// The entry at place e of the sorted list.
+__device__ __forceinline__ uint32_t source_row(const SumK &A, uint32_t val) {
+    return A.per_row == 1 ? val : val / A.per_row;
+}
+
+// Sum of the sorted entries e0 .. e1 - 1 in order, U rows in flight.
+template <int U, typename E>
 __device__ __forceinline__ f8 sum_entries(const SumK &A, const E *X, uint32_t e0, uint32_t e1, int c) {
     f8 sum = f8{};
-    for (uint32_t e = e0; e < e1; e += 4) {
-        f8 v[4];
-        float w[4];
+    for (uint32_t e = e0; e < e1; e += U) {
+        uint32_t val[U];
+        f8 v[U];
+        float w[U];
 #pragma unroll
-        for (int x = 0; x < 4; ++x) {
-            const bool in = e + x < e1;
-            const uint32_t val = A.vals[in ? e + x : e0];
-            w[x] = !in ? 0.f : A.w ? A.w[val] : 1.f;
-            v[x] = load8(X + (int64_t)(val / A.per_row) * A.ldx + c);
+        for (int x = 0; x < U; ++x) val[x] = A.vals[e + x < e1 ? e + x : e0];
+#pragma unroll
+        for (int x = 0; x < U; ++x) {
+            w[x] = A.w ? A.w[val[x]] : 1.f;
+            v[x] = load8(X + (int64_t)source_row(A, val[x]) * A.ldx + c);
         }
 #pragma unroll
-        for (int x = 0; x < 4; ++x)
+        for (int x = 0; x < U; ++x)
             if (e + x < e1) sum += w[x] * v[x];
     }
     return sum;
 }
 
+// The value of the lane `off` lanes away (a power of two), eight at a time.
+__device__ __forceinline__ f8 other_lanes(f8 v, int off) {
+    f8 o;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) o[j] = __shfl_xor(v[j], off, 64);
+    return o;
+}
+
 // The partial sums that a piece of kSumPiece consecutive units (entries, or
 // the pieces of the level below) leaves for the long rows that reach into it:
 // [0] of the row at its first entry, [1] of the row at its last, if another.
+// Four lane groups take a quarter of the piece each, in order, since one would
+// wait for 64 rows after one another.
 template <typename E, int LEVEL>
 __global__ __launch_bounds__(kThreads) void k_sum_pieces(SumK A, const E *X, int64_t pieces) {
-    const int64_t q = ((int64_t)blockIdx.x * kThreads + threadIdx.x) >> A.lanes_log;
-    if (q >= pieces) return;
+    const int64_t g = ((int64_t)blockIdx.x * kThreads + threadIdx.x) >> A.lanes_log, q = g >> 2;
+    if (q >= pieces) return;  // whole pieces leave together
     constexpr int64_t kSpan = LEVEL == 0 ? kSumPiece : kSumPiece * kSumPiece;  // entries of a piece
-    const int lane = threadIdx.x & ((1 << A.lanes_log) - 1), c = lane * 8, k = 8 << A.lanes_log;
+    const int lanes = 1 << A.lanes_log, part = (int)(g & 3);
+    const int c = (threadIdx.x & (lanes - 1)) * 8, k = 8 << A.lanes_log;
     const int64_t first = q * kSpan, last = (first + kSpan < A.entries ? first + kSpan : A.entries) - 1;
     const uint64_t r0 = A.keys[first], r1 = A.keys[last];
     float *out = (LEVEL == 0 ? A.carry0 : A.carry1) + q * 2 * k + c;
@@ -157,16 +174,32 @@ __global__ __launch_bounds__(kThreads) void k_sum_pieces(SumK A, const E *X, int
         if (r >= (uint64_t)A.n || (slot && r1 == r0)) continue;
         const int64_t a = A.ptr[r], b = A.ptr[r + 1];
         if (b - a <= kSpan) continue;
-        const int64_t e0 = a > first ? a : first, e1 = b < last + 1 ? b : last + 1;
+        int64_t e0 = a > first ? a : first, e1 = b < last + 1 ? b : last + 1;
         f8 sum = f8{};
         if constexpr (LEVEL == 0) {
-            sum = sum_entries(A, X, (uint32_t)e0, (uint32_t)e1, c);
+            const int64_t quarter = (e1 - e0 + 3) / 4;
+            const int64_t s0 = e0 + part * quarter < e1 ? e0 + part * quarter : e1;
+            const int64_t s1 = s0 + quarter < e1 ? s0 + quarter : e1;
+            sum = sum_entries<8>(A, X, (uint32_t)s0, (uint32_t)s1, c);
         } else {
-            for (int64_t p = e0 / kSumPiece; p * kSumPiece < e1; ++p)
+            const int64_t p0 = e0 / kSumPiece, p1 = (e1 + kSumPiece - 1) / kSumPiece, quarter = (p1 - p0 + 3) / 4;
+            const int64_t s1 = p0 + (part + 1) * quarter < p1 ? p0 + (part + 1) * quarter : p1;
+#pragma unroll 4
+            for (int64_t p = p0 + part * quarter; p < s1; ++p)
                 sum += load8(A.carry0 + (p * 2 + (a > p * kSumPiece ? 1 : 0)) * k + c);
         }
-        store8(out + slot * k, sum);
+        sum += other_lanes(sum, lanes);
+        sum += other_lanes(sum, 2 * lanes);
+        if (part == 0) store8(out + slot * k, sum);
     }
+}
+
+// The parts' sums of row i.
+__device__ __forceinline__ f8 sum_parts(const SumK &A, int64_t i, int c, int k) {
+    f8 sum = f8{};
+#pragma unroll 4
+    for (int32_t p = 0; p < A.n_parts; ++p) sum += load8(A.parts + p * A.part_stride + i * k + c);
+    return sum;
 }
 
 template <typename E>
@@ -174,20 +207,67 @@ __global__ __launch_bounds__(kThreads) void k_sum_rows(SumK A, const E *X, E *ou
     const int64_t i = ((int64_t)blockIdx.x * kThreads + threadIdx.x) >> A.lanes_log;
     if (i >= A.n) return;
     const int c = (threadIdx.x & ((1 << A.lanes_log) - 1)) * 8, k = 8 << A.lanes_log;
-    f8 sum = f8{};
-    for (int32_t p = 0; p < A.n_parts; ++p) sum += load8(A.parts + p * A.part_stride + i * k + c);
     const uint32_t a = A.entries ? A.ptr[i] : 0u, b = A.entries ? A.ptr[i + 1] : 0u;
+    f8 sum = sum_parts(A, i, c, k);
     if (b - a <= (uint32_t)kSumPiece) {
-        sum += sum_entries(A, X, a, b, c);
+        sum += sum_entries<4>(A, X, a, b, c);
     } else {
         const bool two = A.two_levels && b - a > (uint32_t)(kSumPiece * kSumPiece);
         const float *carry = two ? A.carry1 : A.carry0;
         const int64_t span = two ? kSumPiece * kSumPiece : kSumPiece;
         f8 more = f8{};
-        for (int64_t p = a / span; p * span < b; ++p) more += load8(carry + (p * 2 + (a > p * span ? 1 : 0)) * k + c);
+#pragma unroll 4
+        for (int64_t p = a / span; p < (b + span - 1) / span; ++p)
+            more += load8(carry + (p * 2 + (a > p * span ? 1 : 0)) * k + c);
         sum += more;
     }
     store8(out + i * A.ldo + c, sum * A.scale);
+}
+
+// The same sums without a sort: a wave per row of the table reads the ids of
+// all entries, 64 at a time, and its lane groups take the matching ones in
+// turn.  Few entries only: n times entries comparisons, and a row that all
+// entries name is one wave's work.
+template <typename E>
+__global__ __launch_bounds__(kThreads) void k_sum_scan(SumK A, const int32_t *ids, const float *bias, const E *X,
+                                                       E *out, int32_t *err) {
+    const int64_t i = (int64_t)blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6);
+    if (i >= A.n) return;
+    const int lane = threadIdx.x & 63, lanes = 1 << A.lanes_log, groups = 64 >> A.lanes_log, grp = lane >> A.lanes_log;
+    const int c = (lane & (lanes - 1)) * 8, k = 8 << A.lanes_log;
+    const bool use = !(bias && bias[i] < kExcluded);
+    f8 sum = f8{};
+    bool bad = false;
+    int turn = 0;  // of the groups
+    for (int64_t e0 = 0; e0 < A.entries; e0 += 256) {
+        int32_t id[4];
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+            const int64_t e = e0 + 64 * x + lane;
+            id[x] = e < A.entries ? ids[e] : -1;
+        }
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+            bad |= id[x] < -1 || id[x] >= A.n;
+            uint64_t match = __ballot(use && id[x] == (int32_t)i);
+            while (match) {  // `groups` matches at a time
+                uint32_t mine = ~0u;
+                for (int g = 0; g < groups && match; ++g) {
+                    const uint32_t e = (uint32_t)(e0 + 64 * x) + (uint32_t)__builtin_ctzll(match);
+                    match &= match - 1;
+                    if (((turn + g) & (groups - 1)) == grp) mine = e;
+                }
+                turn += 1;
+                if (mine != ~0u) {
+                    const float w = A.w ? A.w[mine] : 1.f;
+                    sum += w * load8(X + (int64_t)source_row(A, mine) * A.ldx + c);
+                }
+            }
+        }
+    }
+    if (bad && i == 0) err[ERR_RANGE] = 1;
+    for (int off = lanes; off < 64; off <<= 1) sum += other_lanes(sum, off);
+    if (grp == 0) store8(out + i * A.ldo + c, (sum + sum_parts(A, i, c, k)) * A.scale);
 }
 
 int lanes_log_of(int k) {
@@ -224,17 +304,23 @@ void sum_rows(const SumPlan &p, const SumArgs &a, hipStream_t s) {
     A.scale = a.scale;
     A.ldo = a.out.ld;
     const E *X = static_cast<const E *>(a.X.p);
+    E *out = static_cast<E *>(a.out.p);
+    if (p.scan) {
+        k_sum_scan<E><<<ceil_div(p.n, kThreads / 64), kThreads, 0, s>>>(A, a.ids, a.bias, X, out, a.err);
+        TSID_HIP(hipGetLastError());
+        return;
+    }
     if (p.entries > kSumPiece) {
         const int64_t n0 = pieces_of(p.entries, kSumPiece);
-        k_sum_pieces<E, 0><<<ceil_div(n0 << A.lanes_log, kThreads), kThreads, 0, s>>>(A, X, n0);
+        k_sum_pieces<E, 0><<<ceil_div(n0 << (A.lanes_log + 2), kThreads), kThreads, 0, s>>>(A, X, n0);
         TSID_HIP(hipGetLastError());
     }
     if (A.two_levels) {
         const int64_t n1 = pieces_of(p.entries, kSumPiece * kSumPiece);
-        k_sum_pieces<E, 1><<<ceil_div(n1 << A.lanes_log, kThreads), kThreads, 0, s>>>(A, X, n1);
+        k_sum_pieces<E, 1><<<ceil_div(n1 << (A.lanes_log + 2), kThreads), kThreads, 0, s>>>(A, X, n1);
         TSID_HIP(hipGetLastError());
     }
-    k_sum_rows<E><<<ceil_div(p.n << A.lanes_log, kThreads), kThreads, 0, s>>>(A, X, static_cast<E *>(a.out.p));
+    k_sum_rows<E><<<ceil_div(p.n << A.lanes_log, kThreads), kThreads, 0, s>>>(A, X, out);
     TSID_HIP(hipGetLastError());
 }
 
@@ -256,6 +342,8 @@ void launch_lookup(int k, int prec, const Rows &F, const int32_t *ids, float sca
 }
 
 void carve_sum(SumPlan &p, Carve &c) {
+    p.scan = p.entries <= kScanEntries && p.n * p.entries <= kScanCompares;
+    if (p.scan) return;
     for (int x = 0; x < 2; ++x) {
         p.keys[x] = c.take<uint64_t>(p.entries);
         p.vals[x] = c.take<uint32_t>(p.entries);
@@ -267,7 +355,7 @@ void carve_sum(SumPlan &p, Carve &c) {
     p.alt = false;
 }
 
-void launch_sum_sort(SumPlan &p, const int32_t *ids, const float *bias, int32_t *err, hipStream_t s) {
+static void sum_sort(SumPlan &p, const int32_t *ids, const float *bias, int32_t *err, hipStream_t s) {
     if (p.entries <= 0) return;
     const int blocks = (int)std::min<int64_t>(ceil_div(p.entries, kThreads), 2048);
     k_sum_keys<<<blocks, kThreads, 0, s>>>(ids, p.entries, p.n, bias, p.keys[0], p.vals[0], p.sort_scratch,
@@ -279,7 +367,8 @@ void launch_sum_sort(SumPlan &p, const int32_t *ids, const float *bias, int32_t 
     TSID_HIP(hipGetLastError());
 }
 
-void launch_sum_rows(const SumPlan &p, int prec, const SumArgs &a, hipStream_t s) {
+void launch_sum_rows(SumPlan &p, int prec, const SumArgs &a, hipStream_t s) {
+    if (!p.scan || p.n <= 0) sum_sort(p, a.ids, a.bias, a.err, s);  // also reports ids of an empty table
     if (p.n <= 0) return;
     if (prec == TSID_BF16) sum_rows<uint16_t>(p, a, s);
     else sum_rows<float>(p, a, s);
