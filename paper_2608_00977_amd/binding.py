@@ -373,6 +373,7 @@ class Tsid:
         torch.cuda.init()
         handle = stream.cuda_stream if stream is not None else 0
         self.device = device
+        self._device = torch.device("cuda", device)
         self.ctx = tsid_create(device, handle, max_device_bytes)
         self._keep = []  # host buffers of chunks in flight
 
@@ -548,25 +549,31 @@ class Tsid:
     # 16-byte aligned stride.
 
     def _stream(self) -> int:
-        return torch.cuda.current_stream(self.device).cuda_stream
+        # the handle alone: torch.cuda.current_stream() makes a Stream object of it first (2.5 us of a 10 us call)
+        return torch._C._cuda_getCurrentRawStream(self.device)
 
     def _on_device(self, what: str, x: torch.Tensor, dtype=None):
-        if not isinstance(x, torch.Tensor) or x.device.type != "cuda" or x.device.index != self.device:
+        if not isinstance(x, torch.Tensor) or not x.is_cuda or x.get_device() != self.device:
             raise TsidError(E_INVAL, what, f"must be a tensor on cuda:{self.device}")
         if dtype is not None and (x.dtype != dtype or not x.is_contiguous()):
             raise TsidError(E_INVAL, what, f"must be contiguous {dtype}")
 
     def _rows(self, what: str, x: torch.Tensor, like: Optional[torch.Tensor] = None) -> tsid_rows:
         self._on_device(what, x)
-        if x.dim() != 2 or x.dtype not in (torch.float32, torch.bfloat16) or (x.shape[0] and x.stride(1) != 1):
+        shape, dtype = x.shape, x.dtype
+        if len(shape) != 2 or (dtype != torch.bfloat16 and dtype != torch.float32):
             raise TsidError(E_INVAL, what, "must be a 2-d fp32 or bf16 tensor with contiguous rows")
-        if like is not None and (x.dtype != like.dtype or x.shape[1] != like.shape[1]):
+        rows, k = shape
+        ld, step = x.stride()
+        if rows and step != 1:
+            raise TsidError(E_INVAL, what, "must be a 2-d fp32 or bf16 tensor with contiguous rows")
+        if like is not None and (dtype != like.dtype or k != like.shape[1]):
             raise TsidError(E_INVAL, what, "differs in type or rank from the other factors")
-        return tsid_rows(x.data_ptr(), x.shape[0], x.stride(0) if x.shape[0] > 1 else x.shape[1])
+        return tsid_rows(x.data_ptr(), rows, ld if rows > 1 else k)
 
     def _scratch(self, nbytes: int) -> torch.Tensor:
         # +255: the start is moved to a 256-byte boundary
-        return torch.empty(nbytes + 255, dtype=torch.uint8, device=f"cuda:{self.device}")
+        return torch.empty(nbytes + 255, dtype=torch.uint8, device=self._device)
 
     def _head(self, H, F, scale, bias, temperature=1.0) -> tsid_head:
         h, f = self._rows("H", H), self._rows("F", F, H)
@@ -599,7 +606,7 @@ class Tsid:
                 raise TsidError(E_INVAL, what, "must have one value per row of H")
 
     def _new(self, shape, dtype=torch.float32) -> torch.Tensor:
-        return torch.empty(shape, dtype=dtype, device=f"cuda:{self.device}")
+        return torch.empty(shape, dtype=dtype, device=self._device)
 
     def rows_check(self):
         """Waits for the current stream and raises TSID_E_RANGE if a row

@@ -289,8 +289,7 @@ __device__ __forceinline__ float max_halves(float a, float b) {
 
 // The slice and row tile of a workgroup: workgroups go to the 8 XCDs in turn,
 // so that the row tiles which read a slice of F run on one XCD and share its L2.
-__device__ __forceinline__ bool place(int32_t n_slices, int32_t n_tiles, int32_t &slice, int32_t &tile) {
-    const int32_t b = blockIdx.x;
+__device__ __forceinline__ bool place(int32_t b, int32_t n_slices, int32_t n_tiles, int32_t &slice, int32_t &tile) {
     if (n_slices < 8) {
         slice = b / n_tiles;
         tile = b % n_tiles;
@@ -316,7 +315,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_score_pass(ScoreK A) {
     extern __shared__ __align__(16) unsigned char smem[];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, h = lane >> 5;
     int32_t slice, tile;
-    if (!place(A.n_slices, A.n_tiles, slice, tile)) return;
+    if (!place(blockIdx.x, A.n_slices, A.n_tiles, slice, tile)) return;
     const int64_t x0 = (int64_t)tile * (4 * CX * 32) + wave * (CX * 32);  // of this run's rows
     const int64_t i0 = slice * A.slice_items, i1 = std::min<int64_t>(i0 + A.slice_items, A.F.count);
     auto buf = [&](int b) { return reinterpret_cast<uint16_t *>(smem + b * TL::kBytes); };
@@ -604,51 +603,59 @@ __device__ __forceinline__ double across(double v) {
     return __longlong_as_double((long long)((uint64_t)hi << 32 | lo));
 }
 
-__device__ __forceinline__ double block_sum(double v, double *red) {
+// Sum and maximum over a team of 64 or 256 threads.
+template <int TEAM>
+__device__ __forceinline__ double team_sum(double v, double *red) {
 #pragma unroll
     for (int off = 32; off > 0; off >>= 1) v += __shfl_xor(v, off, 64);
+    if constexpr (TEAM == 64) return v;
     __syncthreads();
     if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
     __syncthreads();
     return (red[0] + red[1]) + (red[2] + red[3]);
 }
-__device__ __forceinline__ float block_max(float v, double *red) {
+template <int TEAM>
+__device__ __forceinline__ float team_max(float v, double *red) {
 #pragma unroll
     for (int off = 32; off > 0; off >>= 1) v = fmaxf(v, __shfl_xor(v, off, 64));
+    if constexpr (TEAM == 64) return v;
     __syncthreads();
     if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = (double)v;
     __syncthreads();
     return (float)fmax(fmax(red[0], red[1]), fmax(red[2], red[3]));
 }
 
-// One workgroup per row: the slices' sums joined in fp64, the given items'
-// scores in fp64 (k / 8 lanes each), and the best items.  The best `top` items
+// A row's results by one wave, or by a workgroup where the best items are
+// wanted: the slices' sums joined in fp64, the given items' scores in fp64
+// (k / 8 lanes each), and the best items.  The best `top` items
 // lie in the `top` blocks of 32 whose maxima are largest (an item outside them
 // has `top` better ones), so those blocks and kMargin more, for the rounding of
 // the maxima, are scored again in fp64 and ranked by these scores.  The blocks
 // are found through groups of blocks in the same way.
 template <typename E, int K, bool TOP>
 __global__ __launch_bounds__(kThreads) void k_score_finish(FinishK A) {
-    constexpr int LN = K / 8, NI = kThreads / LN;  // lanes of an item, items at a time
+    constexpr int TEAM = TOP ? kThreads : 64;
+    constexpr int LN = K / 8, NI = TEAM / LN;  // lanes of an item, items at a time
     __shared__ double red[4];
-    const int tid = threadIdx.x, sub = tid % LN;
-    const int64_t row = blockIdx.x, t = A.t0 + row;
+    const int tid = threadIdx.x % TEAM, sub = tid % LN;
+    const int64_t row = (int64_t)blockIdx.x * (kThreads / TEAM) + threadIdx.x / TEAM, t = A.t0 + row;
+    if (row >= A.T) return;  // whole teams
     const E *F = static_cast<const E *>(A.F.p);
     const f8 hv = load8(static_cast<const E *>(A.H.p) + t * A.H.ld + sub * 8);
     // log sum and entropy
     float m = kLeast;
-    for (int q = tid; q < A.n_parts; q += kThreads) m = fmaxf(m, A.part[(int64_t)q * A.T + row].x);
-    m = block_max(m, red);
+    for (int q = tid; q < A.n_parts; q += TEAM) m = fmaxf(m, A.part[(int64_t)q * A.T + row].x);
+    m = team_max<TEAM>(m, red);
     double s = 0.0, e = 0.0;
-    for (int q = tid; q < A.n_parts; q += kThreads) {
+    for (int q = tid; q < A.n_parts; q += TEAM) {
         const float4 p = A.part[(int64_t)q * A.T + row];
         if (p.y == 0.f) continue;
         const double d = (double)p.x - (double)m, f = exp2(d);
         s += (double)p.y * f;
         e += ((double)p.z + (double)p.y * d) * f;
     }
-    s = block_sum(s, red);
-    e = block_sum(e, red);
+    s = team_sum<TEAM>(s, red);
+    e = team_sum<TEAM>(e, red);
     const bool empty = s == 0.0;
     const double lse = empty ? -INFINITY : kLn2 * ((double)m + log2(s));
     if (tid == 0) {
@@ -668,40 +675,69 @@ __global__ __launch_bounds__(kThreads) void k_score_finish(FinishK A) {
         return z * A.scale + (A.F.bias ? (double)A.F.bias[id] * A.bias_scale : 0.0);
     };
     const int32_t *ids = A.ids ? A.ids + t * A.per_row : nullptr;
+    constexpr int NP = sizeof(E) == 2 ? 1 : 3;
+    auto eight = [](const Raw<NP> &r) {
+        if constexpr (NP == 1) return __builtin_convertvector(__builtin_bit_cast(b8, r.w[0]), f8);
+        else return load8(reinterpret_cast<const float *>(r.w));
+    };
+    // rows of items, whatever they are, so that nothing waits for their bias
+    auto row_of = [&](int64_t id) {
+        return load_raw<NP>(F, (id >= 0 && id < A.F.count ? id : 0) * A.F.ld + sub * 8);
+    };
+    // visit(j, id, usable, score) for the listed items, by the LN lanes of each
+    auto listed = [&](auto visit) {
+        if (A.F.count <= 0) {
+            for (int j = tid / LN; j < A.per_row; j += NI) visit(j, (int64_t)ids[j], false, 0.0);
+            return;
+        }
+        constexpr int U = 4;
+        for (int base = 0; base < A.per_row; base += NI * U) {
+            const int j0 = base + tid / LN;
+            Raw<NP> r[U];
+            int64_t id[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) id[u] = j0 + u * NI < A.per_row ? ids[j0 + u * NI] : -1;
+#pragma unroll
+            for (int u = 0; u < U; ++u) r[u] = row_of(id[u]);
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                if (base + u * NI >= A.per_row) break;
+                const bool use = usable(id[u]);
+                const double z = score_of(use ? id[u] : 0, eight(r[u]));
+                if (j0 + u * NI < A.per_row) visit(j0 + u * NI, id[u], use, z);
+            }
+        }
+    };
     if (A.logp) {
-        for (int j = tid / LN; j < A.per_row; j += NI) {
-            const int32_t id = ids[j];
+        listed([&](int j, int64_t id, bool use, double z) {
             float v = 0.f;
-            if (usable(id)) v = (float)(score_of(id, load8(F + (int64_t)id * A.F.ld + sub * 8)) - lse);
+            if (use) v = (float)(z - lse);
             else if (id >= 0 && id < A.F.count) v = -INFINITY;
             else if (id != -1) A.err[ERR_RANGE] = 1;
             if (sub == 0) A.logp[t * A.per_row + j] = v;
-        }
+        });
     }
     if (A.teacher) {
         const float *tl = A.teacher + t * A.per_row;
         float tm = -INFINITY;
-        for (int j = tid; j < A.per_row; j += kThreads) {
+        for (int j = tid; j < A.per_row; j += TEAM) {
             const int32_t id = ids[j];
             if (usable(id)) tm = fmaxf(tm, tl[j]);
             else if (id < -1 || id >= A.F.count) A.err[ERR_RANGE] = 1;
         }
-        tm = block_max(tm, red);
+        tm = team_max<TEAM>(tm, red);
         double w_sum = 0.0, a_sum = 0.0;
         if (tm > -INFINITY) {
-            for (int j = tid / LN; j < A.per_row; j += NI) {
-                const int32_t id = ids[j];
-                if (!usable(id)) continue;
-                const double lw = ((double)tl[j] - (double)tm) / A.tau, w = exp(lw);
-                const double z = score_of(id, load8(F + (int64_t)id * A.F.ld + sub * 8));
+            listed([&](int j, int64_t, bool use, double z) {
+                const double lw = ((double)tl[j] - (double)tm) / A.tau, w = use ? exp(lw) : 0.0;
                 if (sub == 0 && w > 0.0) {
                     w_sum += w;
                     a_sum += w * (lw - (z - lse));
                 }
-            }
+            });
         }
-        w_sum = block_sum(w_sum, red);
-        a_sum = block_sum(a_sum, red);
+        w_sum = team_sum<TEAM>(w_sum, red);
+        a_sum = team_sum<TEAM>(a_sum, red);
         if (tid == 0) A.loss[t] = w_sum > 0.0 ? (float)(A.tau * A.tau * (a_sum / w_sum - log(w_sum))) : 0.f;
     }
     if constexpr (TOP) {
@@ -767,20 +803,20 @@ __global__ __launch_bounds__(kThreads) void k_score_finish(FinishK A) {
         __syncthreads();
         constexpr int U = 8;  // items of a lane group in flight
         for (int j0 = tid / LN; j0 < got * 32; j0 += NI * U) {
-            f8 f[U];
+            Raw<NP> r[U];
             int64_t id[U];
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 const int j = j0 + u * NI;
                 id[u] = j < got * 32 ? (int64_t)pick[0][j >> 5] * 32 + (j & 31) : -1;
-                if (!usable(id[u])) id[u] = -1;
-                f[u] = load8(F + std::max<int64_t>(id[u], 0) * A.F.ld + sub * 8);
+                r[u] = row_of(id[u]);
             }
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 const int j = j0 + u * NI;
-                const double z = score_of(std::max<int64_t>(id[u], 0), f[u]);
-                if (sub == 0 && j < got * 32) cand[j] = id[u] >= 0 ? order_key(z) : 0ull;
+                const bool use = usable(id[u]);
+                const double z = score_of(use ? id[u] : 0, eight(r[u]));
+                if (sub == 0 && j < got * 32) cand[j] = use ? order_key(z) : 0ull;
             }
         }
         __syncthreads();
@@ -862,7 +898,6 @@ __global__ __launch_bounds__(kThreads) void k_head_coef(HeadGrad G, int64_t T, i
 
 struct GradK {
     Side X, Y;
-    int32_t x_items;   // X holds the items (the gradient of F), Y the rows; else the other way round
     float c;
     int turn;
     float bias_c;
@@ -882,13 +917,12 @@ struct GradK {
 // rounded to bf16 for bf16 factors (2^-9 of a term of a sum that is itself
 // rounded to bf16), and split in three parts for fp32 ones.
 template <int K, int NP, int YT, bool ITEMS, bool ENT>
-__global__ __launch_bounds__(kThreads, 2) void k_grad_pass(GradK A) {
+__device__ __forceinline__ void grad_pass(const GradK &A, int32_t block, unsigned char *smem) {
     using S = Shape<K, NP>;
     using TL = Tile<K, NP, YT>;
-    extern __shared__ __align__(16) unsigned char smem[];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, h = lane >> 5;
     int32_t slice, tile;
-    if (!place(A.n_slices, A.n_tiles, slice, tile)) return;
+    if (!place(block, A.n_slices, A.n_tiles, slice, tile)) return;
     const int64_t x0 = (int64_t)tile * 128 + wave * 32, xr = x0 + (lane & 31);
     const int64_t i0 = slice * A.slice_rows, i1 = std::min<int64_t>(i0 + A.slice_rows, A.Y.count);
     auto buf = [&](int b) { return reinterpret_cast<uint16_t *>(smem + b * TL::kBytes); };
@@ -1029,6 +1063,15 @@ __global__ __launch_bounds__(kThreads, 2) void k_grad_pass(GradK A) {
     }
 }
 
+// Both gradients in one launch: the first `h_blocks` workgroups (a multiple of
+// 8, for place()) take the rows' gradients, the others the items'.
+template <int K, int NP, int YT, bool ENT>
+__global__ __launch_bounds__(kThreads, 2) void k_grad_pass(GradK rows, GradK items, int32_t h_blocks) {
+    extern __shared__ __align__(16) unsigned char smem[];
+    if ((int32_t)blockIdx.x < h_blocks) grad_pass<K, NP, YT, false, ENT>(rows, blockIdx.x, smem);
+    else grad_pass<K, NP, YT, true, ENT>(items, blockIdx.x - h_blocks, smem);
+}
+
 // out[t] = scale (a_t * sum of the parts + sum_j w_tj F[id_tj]) (a_t in the
 // parts already: coef null); K / 8 lanes a row, four listed items in flight.
 template <typename E, int K>
@@ -1072,25 +1115,30 @@ constexpr int kCus = 256;
 
 // How a streamed side of `rows` rows is cut: `tiles` workgroups per slice, of
 // which two fit a CU; slices of whole units, a multiple of the 8 XCDs from 8
-// on.  Chosen by the time it takes: rounds of workgroups, each its slice and a
-// start that takes as long as about 96 rows, the last round's uneven end, and `slice_cost`, what a
+// on.  Chosen from up to 8 and from whole rounds by the time it takes: rounds of workgroups, each its slice and a
+// start that takes as long as about 400 rows, the last round's uneven end, and `slice_cost`, what a
 // slice's sums cost to write and add, in rows.
 void slices_of(int64_t rows, int64_t tiles, int64_t unit, double slice_cost, int32_t &n_slices, int64_t &slice_rows) {
     double best = 0.0;
     n_slices = 1;
     slice_rows = unit;
-    for (int64_t ns = 1; ns <= 2048; ns += ns < 8 ? 1 : 8) {
+    constexpr int64_t kSlots = 2 * kCus;
+    tiles = std::max<int64_t>(1, tiles);  // an empty side
+    auto look = [&](int64_t ns) {
+        if (ns >= 8) ns = ns / 8 * 8;
         const int64_t each = std::max<int64_t>(unit, ((rows + ns - 1) / ns + unit - 1) / unit * unit);
         const int64_t used = std::max<int64_t>(1, (rows + each - 1) / each);
-        const double rounds = (double)((used * tiles + 2 * kCus - 1) / (2 * kCus));
-        const double cost = (rounds + 0.3) * ((double)each + 96.0) + (double)used * slice_cost;
-        if (ns == 1 || cost < best) {
+        const double rounds = (double)((used * tiles + kSlots - 1) / kSlots);
+        const double cost = (rounds + 0.15) * ((double)each + 400.0) + (double)used * slice_cost;
+        if (best == 0.0 || cost < best) {
             best = cost;
             n_slices = (int32_t)used;
             slice_rows = each;
         }
-        if (each == unit) break;
-    }
+    };
+    for (int64_t ns = 1; ns <= 8; ++ns) look(ns);
+    for (int64_t r = 1; r <= 8; ++r)  // whole rounds
+        if (kSlots * r / tiles > 8) look(kSlots * r / tiles);
 }
 
 struct ScorePlan {
@@ -1174,28 +1222,19 @@ void launch_score(const ScoreK &a, const ScorePlan &p, hipStream_t s) {
     TSID_HIP(hipGetLastError());
 }
 
-template <int K, int NP, bool ITEMS, bool ENT>
-void launch_grad_pass(const GradK &a, hipStream_t s) {
+template <int K, int NP, bool ENT>
+void launch_grad(const GradK &rows, const GradK &items, hipStream_t s) {
     constexpr int YT = NP == 1 ? 64 : 32;
     constexpr size_t lds = 3 * Tile<K, NP, YT>::kBytes;
-    auto *pass = &k_grad_pass<K, NP, YT, ITEMS, ENT>;
+    auto *pass = &k_grad_pass<K, NP, YT, ENT>;
     if (lds > 64 * 1024) {
         static std::atomic<uint64_t> done;
         allow_lds(reinterpret_cast<const void *>(pass), lds, done);
     }
-    pass<<<grid_of(a.n_slices, a.n_tiles), kThreads, lds, s>>>(a);
+    const int h_blocks = rows.n_tiles ? (grid_of(rows.n_slices, rows.n_tiles) + 7) / 8 * 8 : 0;
+    const int f_blocks = items.n_tiles ? grid_of(items.n_slices, items.n_tiles) : 0;
+    pass<<<h_blocks + f_blocks, kThreads, lds, s>>>(rows, items, h_blocks);
     TSID_HIP(hipGetLastError());
-}
-
-template <int K, int NP>
-void launch_grad(bool items, bool ent, const GradK &a, hipStream_t s) {
-    if (items) {
-        if (ent) launch_grad_pass<K, NP, true, true>(a, s);
-        else launch_grad_pass<K, NP, true, false>(a, s);
-    } else {
-        if (ent) launch_grad_pass<K, NP, false, true>(a, s);
-        else launch_grad_pass<K, NP, false, false>(a, s);
-    }
 }
 
 // f.template operator()<K, NP>() for the rank and precision at hand.
@@ -1262,7 +1301,7 @@ void score_rows(const Head &h, const ScorePlan &p, FinishK f, bool entropy, hipS
         for_rank(h.k, h.prec, [&](auto kk, auto np) {
             using E = std::conditional_t<np() == 1, uint16_t, float>;
             if (f.top > 0) k_score_finish<E, kk(), true><<<(unsigned)a.T, kThreads, 0, s>>>(f);
-            else k_score_finish<E, kk(), false><<<(unsigned)a.T, kThreads, 0, s>>>(f);
+            else k_score_finish<E, kk(), false><<<ceil_div(a.T, kThreads / 64), kThreads, 0, s>>>(f);
         });
         TSID_HIP(hipGetLastError());
     }
@@ -1272,7 +1311,7 @@ struct GradPlan {
     int32_t h_slices, h_tiles, f_slices, f_tiles;
     int64_t h_rows, f_rows;
     float4 *coef;
-    float *w, *part;
+    float *w, *h_part, *f_part;
     SumPlan sum;
 };
 
@@ -1287,8 +1326,8 @@ GradPlan plan_grad(int64_t T, int64_t n, int k, int prec, int n_ids, Carve &c) {
     slices_of(T, p.f_tiles, 64, per_row * (double)n, p.f_slices, p.f_rows);
     p.coef = c.take<float4>(T);
     p.w = c.take<float>(T * n_ids);
-    // the two sides take turns at the same parts
-    p.part = c.take<float>(std::max<int64_t>((int64_t)p.h_slices * T, (int64_t)p.f_slices * n) * k);
+    p.h_part = c.take<float>((int64_t)p.h_slices * T * k);
+    p.f_part = c.take<float>((int64_t)p.f_slices * n * k);
     p.sum.entries = T * n_ids;
     p.sum.n = n;
     p.sum.k = k;
@@ -1356,32 +1395,40 @@ void run_head_grad(const Head &h, const HeadGrad &g, void *ws, int32_t *err, hip
     a.unit = h.prec == TSID_BF16 ? 1.f / a.c : 1.f;
     a.bias_c = (float)((double)h.bias_scale * kLog2e);
     a.coef = p.coef;
-    a.part = p.part;
-    if (g.dH.p && T > 0) {
+    GradK b = a;
+    const bool want_h = g.dH.p && T > 0, want_f = g.dF.p && n > 0;
+    if (want_h) {
         a.X = side_of(h.H, nullptr);
         a.Y = side_of(h.F, h.bias);
         a.slice_rows = p.h_rows;
         a.n_slices = p.h_slices;
         a.n_tiles = p.h_tiles;
-        for_rank(h.k, h.prec, [&](auto kk, auto np) { launch_grad<kk(), np()>(false, ent, a, s); });
+        a.part = p.h_part;
+    }
+    if (want_f && T > 0) {
+        b.X = side_of(h.F, h.bias);
+        b.Y = side_of(h.H, nullptr);
+        b.slice_rows = p.f_rows;
+        b.n_slices = p.f_slices;
+        b.n_tiles = p.f_tiles;
+        b.part = p.f_part;
+    }
+    if (a.n_tiles || b.n_tiles)
+        for_rank(h.k, h.prec, [&](auto kk, auto np) {
+            if (ent) launch_grad<kk(), np(), true>(a, b, s);
+            else launch_grad<kk(), np(), false>(a, b, s);
+        });
+    if (want_h) {
         const float4 *coef = ent ? nullptr : p.coef;
         for_rank(h.k, h.prec, [&](auto kk, auto np) {
             using E = std::conditional_t<np() == 1, uint16_t, float>;
             k_grad_rows<E, kk()><<<ceil_div(T * (kk() / 8), kThreads), kThreads, 0, s>>>(
-                p.part, p.h_slices, T, coef, g.ids, p.w, g.per_row, static_cast<const E *>(h.F.p), h.F.ld, h.scale,
+                p.h_part, p.h_slices, T, coef, g.ids, p.w, g.per_row, static_cast<const E *>(h.F.p), h.F.ld, h.scale,
                 static_cast<E *>(g.dH.p), g.dH.ld);
         });
         TSID_HIP(hipGetLastError());
     }
-    if (g.dF.p && n > 0) {
-        if (T > 0) {
-            a.X = side_of(h.F, h.bias);
-            a.Y = side_of(h.H, nullptr);
-            a.slice_rows = p.f_rows;
-            a.n_slices = p.f_slices;
-            a.n_tiles = p.f_tiles;
-            for_rank(h.k, h.prec, [&](auto kk, auto np) { launch_grad<kk(), np()>(true, ent, a, s); });
-        }
+    if (want_f) {
         SumArgs sa{};
         sa.ids = g.ids;
         sa.bias = h.bias;
@@ -1389,7 +1436,7 @@ void run_head_grad(const Head &h, const HeadGrad &g, void *ws, int32_t *err, hip
         sa.X = h.H;
         sa.w = p.w;
         sa.per_row = std::max(1, g.per_row);
-        sa.parts = p.part;
+        sa.parts = p.f_part;
         sa.n_parts = T > 0 ? p.f_slices : 0;
         sa.part_stride = n * h.k;
         sa.scale = h.scale;

@@ -343,7 +343,10 @@ void launch_lookup(int k, int prec, const Rows &F, const int32_t *ids, float sca
 
 void carve_sum(SumPlan &p, Carve &c) {
     p.scan = p.entries <= kScanEntries && p.n * p.entries <= kScanCompares;
-    if (p.scan) return;
+    if (p.scan) {
+        c.take<uint32_t>(1);  // a size of 0 says that the arguments are wrong
+        return;
+    }
     for (int x = 0; x < 2; ++x) {
         p.keys[x] = c.take<uint64_t>(p.entries);
         p.vals[x] = c.take<uint32_t>(p.entries);
