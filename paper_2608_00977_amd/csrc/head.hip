@@ -664,7 +664,7 @@ __global__ __launch_bounds__(kThreads) void k_score_finish(FinishK A) {
     }
     auto usable = [&](int64_t id) { return id >= 0 && id < A.F.count && !(A.F.bias && A.F.bias[id] < kExcluded); };
     // the score of an item whose factors f the LN lanes hold
-    auto score_of = [&](int64_t id, const f8 &f) {
+    auto score_of = [&](float bias, const f8 &f) {
         double z = 0.0;
 #pragma unroll
         for (int c = 0; c < 8; ++c) z = fma((double)hv[c], (double)f[c], z);
@@ -672,7 +672,7 @@ __global__ __launch_bounds__(kThreads) void k_score_finish(FinishK A) {
         if constexpr (LN >= 4) z += across<0x4E>(z);    // i ^ 2
         if constexpr (LN >= 8) z += across<0x141>(z);   // 7 - i of each 8
         if constexpr (LN >= 16) z += across<0x140>(z);  // 15 - i of each 16
-        return z * A.scale + (A.F.bias ? (double)A.F.bias[id] * A.bias_scale : 0.0);
+        return z * A.scale + (double)bias * A.bias_scale;
     };
     const int32_t *ids = A.ids ? A.ids + t * A.per_row : nullptr;
     constexpr int NP = sizeof(E) == 2 ? 1 : 3;
@@ -680,9 +680,14 @@ __global__ __launch_bounds__(kThreads) void k_score_finish(FinishK A) {
         if constexpr (NP == 1) return __builtin_convertvector(__builtin_bit_cast(b8, r.w[0]), f8);
         else return load8(reinterpret_cast<const float *>(r.w));
     };
-    // rows of items, whatever they are, so that nothing waits for their bias
-    auto row_of = [&](int64_t id) {
-        return load_raw<NP>(F, (id >= 0 && id < A.F.count ? id : 0) * A.F.ld + sub * 8);
+    // an item's row and bias, whatever they are, so that one does not wait for
+    // the other; -inf for what is no item, 0 without a bias
+    auto row_of = [&](int64_t id, float &bias) {
+        const bool in = id >= 0 && id < A.F.count;
+        const int64_t at = in ? id : 0;
+        bias = A.F.bias ? A.F.bias[at] : 0.f;
+        if (!in) bias = -INFINITY;
+        return load_raw<NP>(F, at * A.F.ld + sub * 8);
     };
     // visit(j, id, usable, score) for the listed items, by the LN lanes of each
     auto listed = [&](auto visit) {
@@ -695,15 +700,16 @@ __global__ __launch_bounds__(kThreads) void k_score_finish(FinishK A) {
             const int j0 = base + tid / LN;
             Raw<NP> r[U];
             int64_t id[U];
+            float bias[U];
 #pragma unroll
             for (int u = 0; u < U; ++u) id[u] = j0 + u * NI < A.per_row ? ids[j0 + u * NI] : -1;
 #pragma unroll
-            for (int u = 0; u < U; ++u) r[u] = row_of(id[u]);
+            for (int u = 0; u < U; ++u) r[u] = row_of(id[u], bias[u]);
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 if (base + u * NI >= A.per_row) break;
-                const bool use = usable(id[u]);
-                const double z = score_of(use ? id[u] : 0, eight(r[u]));
+                const bool use = bias[u] >= kExcluded;
+                const double z = score_of(use ? bias[u] : 0.f, eight(r[u]));
                 if (j0 + u * NI < A.per_row) visit(j0 + u * NI, id[u], use, z);
             }
         }
@@ -804,18 +810,17 @@ __global__ __launch_bounds__(kThreads) void k_score_finish(FinishK A) {
         constexpr int U = 8;  // items of a lane group in flight
         for (int j0 = tid / LN; j0 < got * 32; j0 += NI * U) {
             Raw<NP> r[U];
-            int64_t id[U];
+            float bias[U];
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 const int j = j0 + u * NI;
-                id[u] = j < got * 32 ? (int64_t)pick[0][j >> 5] * 32 + (j & 31) : -1;
-                r[u] = row_of(id[u]);
+                r[u] = row_of(j < got * 32 ? (int64_t)pick[0][j >> 5] * 32 + (j & 31) : -1, bias[u]);
             }
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 const int j = j0 + u * NI;
-                const bool use = usable(id[u]);
-                const double z = score_of(use ? id[u] : 0, eight(r[u]));
+                const bool use = bias[u] >= kExcluded;
+                const double z = score_of(use ? bias[u] : 0.f, eight(r[u]));
                 if (sub == 0 && j < got * 32) cand[j] = use ? order_key(z) : 0ull;
             }
         }
