@@ -522,7 +522,8 @@ tsid_status tsid_get_timing(const tsid_ctx *ctx, tsid_timing *out);
  *    gives; its contents need no care before or after, but two calls that may
  *    run at once (other streams, graphs replayed at once) need one each.
  *  - The context's other streams and state are not used, and the calling
- *    thread's current device is left as it was.
+ *    thread's current device is left as it was.  A graph that holds such calls
+ *    is not replayed after tsid_destroy.
  *  - ids are int32.  -1 stands for no item.  Another id outside the table is
  *    treated as -1 and reported as E_RANGE by the next tsid_rows_check.
  *  - Sums are fp32 or fp64 in a fixed order, without atomics: results repeat

@@ -2798,10 +2798,10 @@ Head check_head(const tsid_head *h) {
     o.bias = h->bias;
     o.k = h->k;
     o.prec = h->prec;
-    o.scale = h->scale / h->temperature;
-    if (o.scale != 0.f && !(std::fabs(o.scale) >= 1e-12f && std::fabs(o.scale) <= 1e12f))
+    o.scale = (double)h->scale / (double)h->temperature;
+    if (o.scale != 0.0 && !(std::fabs(o.scale) >= 1e-12 && std::fabs(o.scale) <= 1e12))
         fail(TSID_E_INVAL, "scale / temperature must be 0 or from 1e-12 to 1e12 in size");
-    o.bias_scale = 1.f / h->temperature;
+    o.bias_scale = 1.0 / (double)h->temperature;
     return o;
 }
 

@@ -5,14 +5,22 @@
 // No score ever reaches memory.  Both directions stream tiles of 32 rows of one
 // side (Y) past rows of the other side that stay in registers (X), one wave per
 // 32 or 64 of them, and take S = Y X^T with v_mfma_f32_32x32x16_bf16, which leaves
-// lane l with column l % 32 (its own row of X) and 16 of the 32 rows of Y (rows
-// 8 (r / 4) + 4 (l / 32) + r % 4, r = 0 .. 15): a row's running maximum and sums
-// are the lane's own, without any exchange.
+// lane l with column l % 32 (its own row of X) and 16 of the 32 rows of Y (the
+// matrix unit's rows 8 (r / 4) + 4 (l / 32) + r % 4, r = 0 .. 15): a row's running
+// maximum and sums are the lane's own, without any exchange.
 //
 // fp32 factors are split into three bf16 parts each (8 + 8 + 8 bits, exact) and
 // multiplied part by part, six products for the nine (the other three are below
 // 2^-24 of the whole): 96 cycles of a SIMD per 64 scores at k = 128, where
 // v_mfma_f32_32x32x2_f32 takes 256.  bf16 factors take 16.
+//
+// What bounds the passes (one MI355X, k = 128, bf16; counters).  Scores: vector
+// work, 74 to 77 % of the cycles (an exponential is four issue slots, and with
+// maximum, exponent, sums and entropy a score takes 7.5), beside it the matrix
+// unit at 34 to 44 %: 16,384 x 100 k scores in 0.49 ms, 3.4e12 a second.  Few
+// rows: the table's read, 256 MB in 42 us.  Gradients: matrix unit 56 % and vector
+// work 50 % of the cycles of two waves a SIMD, both sides of 16,384 x 100 k in
+// 1.6 ms, 1.0 PFLOP/s where a large library product reaches 1.3.
 //
 // Exponentials are base 2: p = 2^(c s - m) with c = |scale| log2 e (a negative
 // scale turns the sign of X).
@@ -1263,8 +1271,8 @@ Side side_of(const Rows &r, const float *bias) { return Side{r.p, r.count, r.ld,
 
 // c and the sign of the scores; scale 0 is X = 0 and c = 1.
 void exponent_of(const Head &h, float &c, int &turn) {
-    c = h.scale == 0.f ? 1.f : (float)(std::fabs((double)h.scale) * kLog2e);
-    turn = h.scale == 0.f ? kNone : h.scale < 0.f ? kTurn : kKeep;
+    c = h.scale == 0.0 ? 1.f : (float)(std::fabs(h.scale) * kLog2e);
+    turn = h.scale == 0.0 ? kNone : h.scale < 0.0 ? kTurn : kKeep;
 }
 
 // The pass over all items and the rows' results, a run of rows at a time.
@@ -1273,7 +1281,7 @@ void score_rows(const Head &h, const ScorePlan &p, FinishK f, bool entropy, hipS
     a.H = side_of(h.H, nullptr);
     a.F = side_of(h.F, h.bias);
     exponent_of(h, a.c, a.turn);
-    a.bias_c = (float)((double)h.bias_scale * kLog2e / (double)a.c);
+    a.bias_c = (float)(h.bias_scale * kLog2e / (double)a.c);
     a.off = kOff / a.c;
     a.slice_items = p.slice_items;
     a.n_slices = p.n_slices;
@@ -1398,7 +1406,7 @@ void run_head_grad(const Head &h, const HeadGrad &g, void *ws, int32_t *err, hip
     GradK a{};
     exponent_of(h, a.c, a.turn);
     a.unit = h.prec == TSID_BF16 ? 1.f / a.c : 1.f;
-    a.bias_c = (float)((double)h.bias_scale * kLog2e);
+    a.bias_c = (float)(h.bias_scale * kLog2e);
     a.coef = p.coef;
     GradK b = a;
     const bool want_h = g.dH.p && T > 0, want_f = g.dF.p && n > 0;
@@ -1428,7 +1436,7 @@ void run_head_grad(const Head &h, const HeadGrad &g, void *ws, int32_t *err, hip
         for_rank(h.k, h.prec, [&](auto kk, auto np) {
             using E = std::conditional_t<np() == 1, uint16_t, float>;
             k_grad_rows<E, kk()><<<ceil_div(T * (kk() / 8), kThreads), kThreads, 0, s>>>(
-                p.h_part, p.h_slices, T, coef, g.ids, p.w, g.per_row, static_cast<const E *>(h.F.p), h.F.ld, h.scale,
+                p.h_part, p.h_slices, T, coef, g.ids, p.w, g.per_row, static_cast<const E *>(h.F.p), h.F.ld, (float)h.scale,
                 static_cast<E *>(g.dH.p), g.dH.ld);
         });
         TSID_HIP(hipGetLastError());
@@ -1444,7 +1452,7 @@ void run_head_grad(const Head &h, const HeadGrad &g, void *ws, int32_t *err, hip
         sa.parts = p.f_part;
         sa.n_parts = T > 0 ? p.f_slices : 0;
         sa.part_stride = n * h.k;
-        sa.scale = h.scale;
+        sa.scale = (float)h.scale;
         sa.out = g.dF;
         launch_sum_rows(p.sum, h.prec, sa, s);
     }

@@ -504,7 +504,7 @@ static bool radix_passes(uint64_t *keys, uint32_t *vals, uint64_t *keys_alt, uin
     const int nb = ceil_div(n, kSortTile);
     const int64_t ns = (int64_t)nb * 256;
     State *state = reinterpret_cast<State *>(scratch + kSortCtl);
-    k_radix_hist<State><<<std::min(nb, 512), kThreads, 0, s>>>(keys, n, bit0, passes, scratch, state, ns, unsorted);
+    k_radix_hist<State><<<std::min(ceil_div(n, kSortTile / 4), 512), kThreads, 0, s>>>(keys, n, bit0, passes, scratch, state, ns, unsorted);
     TSID_HIP(hipGetLastError());
     bool alt = false;
     for (int p = 0; p < passes; ++p) {

@@ -81,8 +81,7 @@ struct Head {
     Rows H, F;
     const float *bias;
     int k, prec;
-    float scale;    // already divided by the temperature
-    float bias_scale;  // 1 / temperature
+    double scale, bias_scale;  // both divided by the temperature
 };
 // A bias below this excludes its item: its row of F is never used.
 constexpr float kExcluded = -1e7f;
