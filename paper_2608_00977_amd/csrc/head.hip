@@ -919,7 +919,118 @@ struct GradK {
     int64_t slice_rows;
     int32_t n_slices, n_tiles;
     float *part;       // [slice][rows of X][K]
+    // the listed items' part of the items' gradient, added in the pass (per_row 0: not here)
+    const int32_t *ids;
+    const float *w;
+    int32_t per_row;
 };
+
+// Adds the listed items' part to a workgroup's sums of 128 items: of the
+// entries of its rows y (a slice), w h_y to the item that the entry lists.  The
+// sums go through LDS.  Entries are looked through 1,024 at a time (512 at k =
+// 128, where two workgroups share a CU's LDS); those of these items are listed
+// in order, dealt to eight teams of 32 lanes by their item, and added by them in
+// order, four rows in flight.
+constexpr int listed_at_once(int K) { return K >= 128 ? 512 : 1024; }
+constexpr size_t listed_lds(int K) { return 128 * (size_t)K * 4 + (size_t)listed_at_once(K) * (12 + 8 * 2); }
+
+template <int K, int NP, int NB>
+__device__ __forceinline__ void add_listed(const GradK &A, const f16 (&acc)[NB], int64_t x0, int64_t i0, int64_t i1,
+                                           int32_t slice, unsigned char *smem, uint32_t *wave_count) {
+    constexpr int kListed = listed_at_once(K), P = kListed / kThreads;
+    float *sum = reinterpret_cast<float *>(smem);  // [128][K]
+    int32_t *item = reinterpret_cast<int32_t *>(sum + 128 * K);
+    uint32_t *row = reinterpret_cast<uint32_t *>(item + kListed);
+    float *weight = reinterpret_cast<float *>(row + kListed);
+    uint16_t *mine = reinterpret_cast<uint16_t *>(weight + kListed);  // [8][kListed]
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, h = lane >> 5;
+    __syncthreads();  // the tiles of Y are done with
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) {
+        const int c = nb * 16 + (lane >> 4 & 1) * (NB * 16) + (lane & 15);
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+            if (c < K) sum[(wave * 32 + 8 * (r / 4) + r % 4 + 4 * h) * K + c] = acc[nb][r];
+    }
+    const int team = tid >> 5, tl = tid & 31, c = 4 * tl;
+    const uint64_t below = (uint64_t(1) << lane) - 1;
+    const int64_t e_end = std::min<int64_t>(i1, A.Y.count) * A.per_row;
+    for (int64_t e0 = i0 * A.per_row; e0 < e_end; e0 += kListed) {
+        int64_t local[P];
+        float w[P];
+        uint32_t at = 0, hits = 0, count = 0;
+#pragma unroll
+        for (int q = 0; q < P; ++q) {
+            const int64_t e = e0 + P * tid + q;
+            local[q] = e < e_end ? (int64_t)A.ids[e] - x0 : -1;
+        }
+#pragma unroll
+        for (int q = 0; q < P; ++q) {
+            w[q] = local[q] >= 0 && local[q] < 128 ? A.w[e0 + P * tid + q] : 0.f;  // 0: also an entry that is no item's
+            const uint64_t hit = __ballot(w[q] != 0.f);
+            at += (uint32_t)__popcll(hit & below);
+            hits += (uint32_t)__popcll(hit);
+        }
+        if (lane == 0) wave_count[wave] = hits;
+        __syncthreads();
+        for (int v = 0; v < 4; ++v) {
+            if (v < wave) at += wave_count[v];
+            count += wave_count[v];
+        }
+#pragma unroll
+        for (int q = 0; q < P; ++q) {
+            if (w[q] != 0.f) {
+                item[at] = (int32_t)local[q];
+                row[at] = (uint32_t)(e0 + P * tid + q) / (uint32_t)A.per_row;
+                weight[at] = w[q];
+                ++at;
+            }
+        }
+        __syncthreads();
+        uint32_t n_mine = 0;
+        for (uint32_t j0 = 0; j0 < count; j0 += 32) {
+            const uint32_t j = j0 + tl;
+            const uint64_t b = __ballot(j < count && (item[j < count ? j : 0] & 7) == team);
+            const uint32_t half = (uint32_t)(b >> (32 * h));
+            if (half >> tl & 1u) mine[team * kListed + n_mine + __popc(half & ((1u << tl) - 1u))] = (uint16_t)j;
+            n_mine += __popc(half);
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        if (c < K) {
+            for (uint32_t j = 0; j < n_mine; j += 4) {
+                f4 y[4];
+                uint32_t m[4];
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    m[q] = mine[team * kListed + std::min<uint32_t>(j + q, n_mine - 1)];
+                    const int64_t from = (int64_t)row[m[q]] * A.Y.ld + c;
+                    if constexpr (NP == 1) {
+                        typedef __bf16 b4 __attribute__((ext_vector_type(4)));
+                        y[q] = __builtin_convertvector(
+                            __builtin_bit_cast(b4, *reinterpret_cast<const uint2 *>(static_cast<const uint16_t *>(A.Y.p) + from)), f4);
+                    } else {
+                        y[q] = *reinterpret_cast<const f4 *>(static_cast<const float *>(A.Y.p) + from);
+                    }
+                }
+#pragma unroll
+                for (int q = 0; q < 4; ++q)
+                    if (j + q < n_mine) {
+                        f4 *s = reinterpret_cast<f4 *>(sum + item[m[q]] * K + c);
+                        *s += weight[m[q]] * y[q];
+                    }
+            }
+        }
+        __syncthreads();  // before the list is written anew
+    }
+    __syncthreads();
+    for (int j = tid; j < 128 * K / 4; j += kThreads) {
+        const int64_t x = x0 + j / (K / 4);
+        if (x < A.X.count)
+            *reinterpret_cast<f4 *>(A.part + ((int64_t)slice * A.X.count + x) * K + j % (K / 4) * 4) =
+                reinterpret_cast<const f4 *>(sum)[j];
+    }
+}
 
 // part[slice][x] = sum over the slice's rows y of g(x, y) y, with
 // g = p a + p log2 p b (ITEMS: a and b of the row y; else of the row x, where a
@@ -930,7 +1041,7 @@ struct GradK {
 // rounded to bf16 for bf16 factors (2^-9 of a term of a sum that is itself
 // rounded to bf16), and split in three parts for fp32 ones.
 template <int K, int NP, int YT, bool ITEMS, bool ENT>
-__device__ __forceinline__ void grad_pass(const GradK &A, int32_t block, unsigned char *smem) {
+__device__ __forceinline__ void grad_pass(const GradK &A, int32_t block, unsigned char *smem, uint32_t *wave_count) {
     using S = Shape<K, NP>;
     using TL = Tile<K, NP, YT>;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, h = lane >> 5;
@@ -1065,6 +1176,12 @@ __device__ __forceinline__ void grad_pass(const GradK &A, int32_t block, unsigne
             cur = nxt;
         }
     }
+    if constexpr (ITEMS) {
+        if (A.per_row > 0) {
+            add_listed<K, NP>(A, acc, (int64_t)tile * 128, i0, i1, slice, smem, wave_count);
+            return;
+        }
+    }
 #pragma unroll
     for (int nb = 0; nb < S::NB; ++nb) {
         const int c = nb * 16 + (grp & 1) * (S::KW / 2) + gi;
@@ -1081,8 +1198,9 @@ __device__ __forceinline__ void grad_pass(const GradK &A, int32_t block, unsigne
 template <int K, int NP, int YT, bool ENT>
 __global__ __launch_bounds__(kThreads, 2) void k_grad_pass(GradK rows, GradK items, int32_t h_blocks) {
     extern __shared__ __align__(16) unsigned char smem[];
-    if ((int32_t)blockIdx.x < h_blocks) grad_pass<K, NP, YT, false, ENT>(rows, blockIdx.x, smem);
-    else grad_pass<K, NP, YT, true, ENT>(items, blockIdx.x - h_blocks, smem);
+    __shared__ uint32_t wave_count[4];
+    if ((int32_t)blockIdx.x < h_blocks) grad_pass<K, NP, YT, false, ENT>(rows, blockIdx.x, smem, wave_count);
+    else grad_pass<K, NP, YT, true, ENT>(items, blockIdx.x - h_blocks, smem, wave_count);
 }
 
 // out[t] = scale (a_t * sum of the parts + sum_j w_tj F[id_tj]) (a_t in the
@@ -1238,11 +1356,12 @@ void launch_score(const ScoreK &a, const ScorePlan &p, hipStream_t s) {
 template <int K, int NP, bool ENT>
 void launch_grad(const GradK &rows, const GradK &items, hipStream_t s) {
     constexpr int YT = NP == 1 ? 64 : 32;
-    constexpr size_t lds = 3 * Tile<K, NP, YT>::kBytes;
+    constexpr size_t tiles = 3 * Tile<K, NP, YT>::kBytes, most = std::max(tiles, listed_lds(K));
+    const size_t lds = items.n_tiles && items.per_row > 0 ? most : tiles;
     auto *pass = &k_grad_pass<K, NP, YT, ENT>;
-    if (lds > 64 * 1024) {
+    if (most > 64 * 1024) {
         static std::atomic<uint64_t> done;
-        allow_lds(reinterpret_cast<const void *>(pass), lds, done);
+        allow_lds(reinterpret_cast<const void *>(pass), most, done);
     }
     const int h_blocks = rows.n_tiles ? (grid_of(rows.n_slices, rows.n_tiles) + 7) / 8 * 8 : 0;
     const int f_blocks = items.n_tiles ? grid_of(items.n_slices, items.n_tiles) : 0;
@@ -1325,8 +1444,16 @@ struct GradPlan {
     int64_t h_rows, f_rows;
     float4 *coef;
     float *w, *h_part, *f_part;
+    bool in_pass;  // the listed items' part of dF is added in the pass
     SumPlan sum;
 };
+
+// Ids that all workgroups of the items' gradient together look through at most
+// for the listed items' part; beyond, the entries are sorted, which costs seven
+// more launches.  4,096 rows with 20 listed of 8,192 items (5.2 M looked at): 199
+// us in the pass, 230 with the sort; 611 rows, 18 of 16,733 items: 81 and 118;
+// 16,384 rows, 50 of 100 k items (640 M) stay with the sort.
+constexpr int64_t kInPass = int64_t(1) << 24;
 
 GradPlan plan_grad(int64_t T, int64_t n, int k, int prec, int n_ids, Carve &c) {
     GradPlan p{};
@@ -1341,7 +1468,8 @@ GradPlan plan_grad(int64_t T, int64_t n, int k, int prec, int n_ids, Carve &c) {
     p.w = c.take<float>(T * n_ids);
     p.h_part = c.take<float>((int64_t)p.h_slices * T * k);
     p.f_part = c.take<float>((int64_t)p.f_slices * n * k);
-    p.sum.entries = T * n_ids;
+    p.in_pass = T * n_ids > 0 && (int64_t)p.f_tiles * T * n_ids <= kInPass;
+    p.sum.entries = p.in_pass ? 0 : T * n_ids;
     p.sum.n = n;
     p.sum.k = k;
     carve_sum(p.sum, c);
@@ -1425,6 +1553,11 @@ void run_head_grad(const Head &h, const HeadGrad &g, void *ws, int32_t *err, hip
         b.n_slices = p.f_slices;
         b.n_tiles = p.f_tiles;
         b.part = p.f_part;
+        if (p.in_pass) {
+            b.ids = g.ids;
+            b.w = p.w;
+            b.per_row = g.per_row;
+        }
     }
     if (a.n_tiles || b.n_tiles)
         for_rank(h.k, h.prec, [&](auto kk, auto np) {

@@ -51,8 +51,8 @@ struct SumPlan {
 // a row is summed in pieces.
 constexpr int kSumPiece = 64;
 // Entries, and comparisons of ids, up to which every row looks through all
-// ids: the sort and what follows it cost six launches and about 35 us, the
-// scan one launch and about 10 us at these bounds.
+// ids: 500 entries into 8,192 rows of 32 take 11 us in one launch, 34 with the
+// sort and the launches that follow it.
 constexpr int64_t kScanEntries = 2048, kScanCompares = int64_t(1) << 27;
 void carve_sum(SumPlan &p, Carve &c);
 // out[i] = scale * (sum of the entries of i + sum of the parts' rows i), every
