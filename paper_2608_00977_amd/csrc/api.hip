@@ -2779,13 +2779,6 @@ void check_array(const void *p, int64_t count, const char *what) {
     if (reinterpret_cast<uintptr_t>(p) % 4 != 0) fail(TSID_E_INVAL, std::string(what) + " must be 4-byte aligned");
 }
 
-void check_workspace(const void *ws, size_t bytes, size_t needed) {
-    if (!ws || reinterpret_cast<uintptr_t>(ws) % 256 != 0)
-        fail(TSID_E_INVAL, "the workspace must be 256-byte aligned device memory");
-    if (bytes < needed)
-        fail(TSID_E_INVAL, "the workspace has " + std::to_string(bytes) + " bytes of " + std::to_string(needed));
-}
-
 Head check_head(const tsid_head *h) {
     if (!h) fail(TSID_E_INVAL, "head is NULL");
     check_rank_prec(h->k, h->prec);
@@ -2810,9 +2803,8 @@ void check_listed(const Head &h, const int32_t *ids, int32_t n_ids) {
     check_array(ids, h.H.count * n_ids, "ids");
 }
 
-// Common part of the gradients: the outputs' tables and the workspace.
-void check_grads(const Head &h, const tsid_head *head, int32_t n_ids, const tsid_rows *dH, const tsid_rows *dF,
-                 const void *ws, size_t bytes, HeadGrad &g) {
+// Common part of the gradients: the outputs' tables.
+void check_grads(const Head &h, const tsid_head *head, const tsid_rows *dH, const tsid_rows *dF, HeadGrad &g) {
     if (dH) {
         g.dH = check_rows(dH, head->k, head->prec, "dH");
         if (g.dH.count != h.H.count) fail(TSID_E_INVAL, "dH must have the rows of H");
@@ -2821,7 +2813,6 @@ void check_grads(const Head &h, const tsid_head *head, int32_t n_ids, const tsid
         g.dF = check_rows(dF, head->k, head->prec, "dF");
         if (g.dF.count != h.F.count) fail(TSID_E_INVAL, "dF must have the rows of F");
     }
-    check_workspace(ws, bytes, head_grad_workspace(h.H.count, h.F.count, h.k, h.prec, n_ids));
 }
 
 bool sizes_ok(int64_t T, int64_t n, int32_t k) { return T >= 0 && T <= kMaxRows && n >= 0 && n <= kMaxRows && valid_rank(k); }
@@ -3115,7 +3106,6 @@ tsid_status tsid_score(tsid_ctx *c, const tsid_head *head, const int32_t *ids, i
         for (const void *p : {(const void *)lse, (const void *)logp, (const void *)entropy, (const void *)top_ids,
                               (const void *)top_logp})
             check_array(p, 0, "an output");
-        check_workspace(ws, ws_bytes, score_workspace(h.H.count, h.F.count, h.k, h.prec, top));
         ScoreOut o{};
         o.ids = ids;
         o.per_row = n_ids;
@@ -3125,7 +3115,7 @@ tsid_status tsid_score(tsid_ctx *c, const tsid_head *head, const int32_t *ids, i
         o.entropy = entropy;
         o.top_ids = top_ids;
         o.top_logp = top_logp;
-        run_score(h, o, ws, c->rows_err, static_cast<hipStream_t>(hip_stream));
+        run_score(h, o, ws, ws_bytes, c->rows_err, static_cast<hipStream_t>(hip_stream));
     });
 }
 
@@ -3152,8 +3142,8 @@ tsid_status tsid_score_grad(tsid_ctx *c, const tsid_head *head, const int32_t *i
         g.dlogp = dlogp;
         g.entropy = entropy;
         g.dentropy = dentropy;
-        check_grads(h, head, n_ids, dH, dF, ws, ws_bytes, g);
-        run_head_grad(h, g, ws, c->rows_err, static_cast<hipStream_t>(hip_stream));
+        check_grads(h, head, dH, dF, g);
+        run_head_grad(h, g, ws, ws_bytes, c->rows_err, static_cast<hipStream_t>(hip_stream));
     });
 }
 
@@ -3166,7 +3156,6 @@ tsid_status tsid_distill(tsid_ctx *c, const tsid_head *head, const int32_t *ids,
         check_array(teacher, h.H.count * n_ids, "teacher");
         check_array(loss, h.H.count, "loss");
         check_array(lse, h.H.count, "lse");
-        check_workspace(ws, ws_bytes, score_workspace(h.H.count, h.F.count, h.k, h.prec, 0));
         DistillOut o{};
         o.ids = ids;
         o.per_row = n_ids;
@@ -3174,7 +3163,7 @@ tsid_status tsid_distill(tsid_ctx *c, const tsid_head *head, const int32_t *ids,
         o.temperature = head->temperature;
         o.loss = loss;
         o.lse = lse;
-        run_distill(h, o, ws, c->rows_err, static_cast<hipStream_t>(hip_stream));
+        run_distill(h, o, ws, ws_bytes, c->rows_err, static_cast<hipStream_t>(hip_stream));
     });
 }
 
@@ -3195,8 +3184,8 @@ tsid_status tsid_distill_grad(tsid_ctx *c, const tsid_head *head, const int32_t 
         g.teacher = teacher;
         g.dloss = dloss;
         g.temperature = head->temperature;
-        check_grads(h, head, n_ids, dH, dF, ws, ws_bytes, g);
-        run_head_grad(h, g, ws, c->rows_err, static_cast<hipStream_t>(hip_stream));
+        check_grads(h, head, dH, dF, g);
+        run_head_grad(h, g, ws, ws_bytes, c->rows_err, static_cast<hipStream_t>(hip_stream));
     });
 }
 

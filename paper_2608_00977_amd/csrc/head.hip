@@ -507,7 +507,7 @@ constexpr int kMargin = 8;        // blocks beyond the wanted best items that ar
 constexpr int kMaxPick = TSID_MAX_TOP + kMargin;
 constexpr int kSelCap = kMaxPick * 32;  // candidates chosen from at a time: the items of the picked blocks
 constexpr int kMaxGroups = 2048;        // one round of them
-static_assert(kMaxGroups <= kSelCap && kMaxPick <= kThreads, "");
+static_assert(kMaxGroups <= kSelCap && kMaxPick <= 256, "");
 
 // Larger floats have larger keys; NaN is below everything.
 __device__ __forceinline__ uint32_t order_key(float v) {
@@ -522,42 +522,53 @@ __device__ __forceinline__ uint64_t order_key(double v) {
 }
 
 struct SelectLds {
-    uint32_t best[kThreads];
-    uint32_t found;
+    uint32_t best[512];
+    uint32_t found, bound;
     uint16_t place[kSelCap];
     int32_t out[kMaxPick];
 };
 
 // The `want` (at most kMaxPick) largest of key[0 .. N - 1] (N <= kSelCap), equal
 // keys in order of place: thread j < min(want, N) returns the place of the
-// j-th, the others -1.  Of the best upper half of each thread's share the
-// want-th largest is a bound that at least `want` keys reach (found bit by
-// bit, every wave for itself); the keys that reach it, hardly more, are ranked
-// by counting.
+// j-th, the others -1.  The keys are dealt to 256 shares; of the best upper half
+// of each share the want-th largest is a bound that at least `want` keys reach
+// (found bit by bit, by one wave: all waves of a large team would wait for one
+// another's issue slots).  The keys that reach it, hardly more, are ranked by
+// counting.
+template <int TEAM>
 __device__ int32_t select_largest(const uint64_t *key, int N, int want, SelectLds &L) {
-    const int t = threadIdx.x, lane = t & 63;
+    const int t = threadIdx.x;
     if (want > N) want = N;
     uint32_t best = 0u;
-    for (int j = t; j < N; j += kThreads) best = max(best, (uint32_t)(key[j] >> 32));
+    for (int j = t; j < N; j += TEAM) best = max(best, (uint32_t)(key[j] >> 32));
     L.best[t] = best;
     if (t == 0) L.found = 0u;
     __syncthreads();
-    uint32_t four[4], bound = 0u;
+    if (t < 64) {
+        uint32_t share[4], bound = 0u;
 #pragma unroll
-    for (int q = 0; q < 4; ++q) four[q] = L.best[64 * q + lane];
-    for (int bit = 31; bit >= 0; --bit) {
-        const uint32_t with = bound | 1u << bit;
-        int reach = 0;
+        for (int q = 0; q < 4; ++q) {
+            share[q] = L.best[64 * q + t];
 #pragma unroll
-        for (int q = 0; q < 4; ++q) reach += __popcll(__ballot(four[q] >= with));
-        if (reach >= want) bound = with;
+            for (int w = 256; w < TEAM; w += 256) share[q] = max(share[q], L.best[w + 64 * q + t]);
+        }
+        for (int bit = 31; bit >= 0; --bit) {
+            const uint32_t with = bound | 1u << bit;
+            int reach = 0;
+#pragma unroll
+            for (int q = 0; q < 4; ++q) reach += __popcll(__ballot(share[q] >= with));
+            if (reach >= want) bound = with;
+        }
+        if (t == 0) L.bound = bound;
     }
-    for (int j = t; j < N; j += kThreads) {
+    __syncthreads();
+    const uint32_t bound = L.bound;
+    for (int j = t; j < N; j += TEAM) {
         if ((uint32_t)(key[j] >> 32) >= bound) L.place[atomicAdd(&L.found, 1u)] = (uint16_t)j;
     }
     __syncthreads();
     const int have = (int)L.found;
-    for (int q = t; q < have; q += kThreads) {
+    for (int q = t; q < have; q += TEAM) {
         const int32_t p = L.place[q];
         const uint64_t k = key[p];
         int rank = 0;
@@ -611,7 +622,7 @@ __device__ __forceinline__ double across(double v) {
     return __longlong_as_double((long long)((uint64_t)hi << 32 | lo));
 }
 
-// Sum and maximum over a team of 64 or 256 threads.
+// Sum and maximum over a team of TEAM threads.
 template <int TEAM>
 __device__ __forceinline__ double team_sum(double v, double *red) {
 #pragma unroll
@@ -620,7 +631,9 @@ __device__ __forceinline__ double team_sum(double v, double *red) {
     __syncthreads();
     if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
     __syncthreads();
-    return (red[0] + red[1]) + (red[2] + red[3]);
+    v = red[0];
+    for (int q = 1; q < TEAM / 64; ++q) v += red[q];
+    return v;
 }
 template <int TEAM>
 __device__ __forceinline__ float team_max(float v, double *red) {
@@ -630,23 +643,27 @@ __device__ __forceinline__ float team_max(float v, double *red) {
     __syncthreads();
     if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = (double)v;
     __syncthreads();
-    return (float)fmax(fmax(red[0], red[1]), fmax(red[2], red[3]));
+    v = (float)red[0];
+    for (int q = 1; q < TEAM / 64; ++q) v = fmaxf(v, (float)red[q]);
+    return v;
 }
 
-// A row's results by one wave, or by a workgroup where the best items are
-// wanted: the slices' sums joined in fp64, the given items' scores in fp64
+// A row's results by one wave (TEAM 64), or by a workgroup where the best items
+// are wanted (256 threads; 512 for few rows, which leave the CUs to them: one row of
+// 1 M items 68 us instead of 73, with 1,024 threads 69, 257 rows 39, 40 and 53): the slices' sums joined in fp64, the given items' scores in fp64
 // (k / 8 lanes each), and the best items.  The best `top` items
 // lie in the `top` blocks of 32 whose maxima are largest (an item outside them
 // has `top` better ones), so those blocks and kMargin more, for the rounding of
 // the maxima, are scored again in fp64 and ranked by these scores.  The blocks
 // are found through groups of blocks in the same way.
-template <typename E, int K, bool TOP>
-__global__ __launch_bounds__(kThreads) void k_score_finish(FinishK A) {
-    constexpr int TEAM = TOP ? kThreads : 64;
+template <typename E, int K, int TEAM>
+__global__ __launch_bounds__(TEAM == 64 ? kThreads : TEAM) void k_score_finish(FinishK A) {
+    constexpr bool TOP = TEAM > 64;
+    constexpr int kTeams = TOP ? 1 : kThreads / TEAM;
     constexpr int LN = K / 8, NI = TEAM / LN;  // lanes of an item, items at a time
-    __shared__ double red[4];
+    __shared__ double red[TEAM / 64];
     const int tid = threadIdx.x % TEAM, sub = tid % LN;
-    const int64_t row = (int64_t)blockIdx.x * (kThreads / TEAM) + threadIdx.x / TEAM, t = A.t0 + row;
+    const int64_t row = (int64_t)blockIdx.x * kTeams + threadIdx.x / TEAM, t = A.t0 + row;
     if (row >= A.T) return;  // whole teams
     const E *F = static_cast<const E *>(A.F.p);
     const f8 hv = load8(static_cast<const E *>(A.H.p) + t * A.H.ld + sub * 8);
@@ -765,7 +782,7 @@ __global__ __launch_bounds__(kThreads) void k_score_finish(FinishK A) {
             int64_t next = 0;
             do {
                 const int n_new = (int)std::min<int64_t>(kSelCap - have, total - next);
-                for (int j = tid; j < n_new; j += kThreads) {
+                for (int j = tid; j < n_new; j += TEAM) {
                     float v;
                     int32_t p;
                     get(next + j, v, p);
@@ -773,7 +790,7 @@ __global__ __launch_bounds__(kThreads) void k_score_finish(FinishK A) {
                 }
                 __syncthreads();
                 next += n_new;
-                const int32_t place = select_largest(cand, have + n_new, want, L);
+                const int32_t place = select_largest<TEAM>(cand, have + n_new, want, L);
                 have = std::min(have + n_new, want);
                 const uint64_t c = place >= 0 ? cand[place] : 0;
                 __syncthreads();
@@ -833,7 +850,7 @@ __global__ __launch_bounds__(kThreads) void k_score_finish(FinishK A) {
             }
         }
         __syncthreads();
-        const int32_t place = select_largest(cand, got * 32, A.top, L);
+        const int32_t place = select_largest<TEAM>(cand, got * 32, A.top, L);
         if (tid < A.top) {
             int32_t id = -1;
             float lp = -INFINITY;
@@ -1432,8 +1449,9 @@ void score_rows(const Head &h, const ScorePlan &p, FinishK f, bool entropy, hipS
         });
         for_rank(h.k, h.prec, [&](auto kk, auto np) {
             using E = std::conditional_t<np() == 1, uint16_t, float>;
-            if (f.top > 0) k_score_finish<E, kk(), true><<<(unsigned)a.T, kThreads, 0, s>>>(f);
-            else k_score_finish<E, kk(), false><<<ceil_div(a.T, kThreads / 64), kThreads, 0, s>>>(f);
+            if (f.top <= 0) k_score_finish<E, kk(), 64><<<ceil_div(a.T, kThreads / 64), kThreads, 0, s>>>(f);
+            else if (a.T > 2 * kCus) k_score_finish<E, kk(), 256><<<(unsigned)a.T, 256, 0, s>>>(f);
+            else k_score_finish<E, kk(), 512><<<(unsigned)a.T, 512, 0, s>>>(f);
         });
         TSID_HIP(hipGetLastError());
     }
@@ -1484,10 +1502,11 @@ size_t score_workspace(int64_t T, int64_t n, int k, int prec, int top) {
     return c.used;
 }
 
-void run_score(const Head &h, const ScoreOut &o, void *ws, int32_t *err, hipStream_t s) {
-    if (h.H.count <= 0) return;
+void run_score(const Head &h, const ScoreOut &o, void *ws, size_t bytes, int32_t *err, hipStream_t s) {
     Carve c{static_cast<char *>(ws)};
     const ScorePlan p = plan_score(h.H.count, h.F.count, h.prec, o.top, c);
+    check_workspace(ws, bytes, c.used);
+    if (h.H.count <= 0) return;
     FinishK f{};
     f.ids = o.ids;
     f.per_row = o.per_row;
@@ -1501,10 +1520,11 @@ void run_score(const Head &h, const ScoreOut &o, void *ws, int32_t *err, hipStre
     score_rows(h, p, f, o.entropy != nullptr, s);
 }
 
-void run_distill(const Head &h, const DistillOut &o, void *ws, int32_t *err, hipStream_t s) {
-    if (h.H.count <= 0) return;
+void run_distill(const Head &h, const DistillOut &o, void *ws, size_t bytes, int32_t *err, hipStream_t s) {
     Carve c{static_cast<char *>(ws)};
     const ScorePlan p = plan_score(h.H.count, h.F.count, h.prec, 0, c);
+    check_workspace(ws, bytes, c.used);
+    if (h.H.count <= 0) return;
     FinishK f{};
     f.ids = o.ids;
     f.per_row = o.per_row;
@@ -1522,10 +1542,11 @@ size_t head_grad_workspace(int64_t T, int64_t n, int k, int prec, int per_row) {
     return c.used;
 }
 
-void run_head_grad(const Head &h, const HeadGrad &g, void *ws, int32_t *err, hipStream_t s) {
+void run_head_grad(const Head &h, const HeadGrad &g, void *ws, size_t bytes, int32_t *err, hipStream_t s) {
     const int64_t T = h.H.count, n = h.F.count;
     Carve c{static_cast<char *>(ws)};
     GradPlan p = plan_grad(T, n, h.k, h.prec, g.per_row, c);
+    check_workspace(ws, bytes, c.used);
     const bool ent = g.dentropy != nullptr;
     if (T > 0) {
         k_head_coef<<<ceil_div(T, 4), kThreads, 0, s>>>(g, T, n, h.bias, p.coef, p.w, err);

@@ -21,6 +21,9 @@ struct Carve {
     }
 };
 
+// E_INVAL unless ws is 256-byte aligned and holds `needed` bytes (before any launch).
+void check_workspace(const void *ws, size_t bytes, size_t needed);
+
 // Rows of a factor table: fp32 or bf16, k per row, ld elements from row to row.
 struct Rows {
     void *p;
@@ -94,7 +97,7 @@ struct ScoreOut {
     float *top_logp;
 };
 size_t score_workspace(int64_t T, int64_t n, int k, int prec, int top);
-void run_score(const Head &h, const ScoreOut &o, void *ws, int32_t *err, hipStream_t s);
+void run_score(const Head &h, const ScoreOut &o, void *ws, size_t bytes, int32_t *err, hipStream_t s);
 
 // dz_ti = (a_t + b_t log p_ti) p_ti + sum_j c_tj [i = id_tj].
 struct HeadGrad {
@@ -109,7 +112,7 @@ struct HeadGrad {
     Rows dH, dF;  // p null: not wanted
 };
 size_t head_grad_workspace(int64_t T, int64_t n, int k, int prec, int per_row);
-void run_head_grad(const Head &h, const HeadGrad &g, void *ws, int32_t *err, hipStream_t s);
+void run_head_grad(const Head &h, const HeadGrad &g, void *ws, size_t bytes, int32_t *err, hipStream_t s);
 
 struct DistillOut {
     const int32_t *ids;
@@ -118,6 +121,6 @@ struct DistillOut {
     float temperature;
     float *loss, *lse;
 };
-void run_distill(const Head &h, const DistillOut &o, void *ws, int32_t *err, hipStream_t s);
+void run_distill(const Head &h, const DistillOut &o, void *ws, size_t bytes, int32_t *err, hipStream_t s);
 
 }  // namespace tsid

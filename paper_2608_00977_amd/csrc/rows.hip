@@ -385,6 +385,13 @@ void launch_lookup(int k, int prec, const Rows &F, const int32_t *ids, float sca
     TSID_HIP(hipGetLastError());
 }
 
+void check_workspace(const void *ws, size_t bytes, size_t needed) {
+    if (!ws || reinterpret_cast<uintptr_t>(ws) % 256 != 0)
+        fail(TSID_E_INVAL, "the workspace must be 256-byte aligned device memory");
+    if (bytes < needed)
+        fail(TSID_E_INVAL, "the workspace has " + std::to_string(bytes) + " bytes of " + std::to_string(needed));
+}
+
 void carve_sum(SumPlan &p, Carve &c) {
     p.scan = p.entries > 0 && p.entries <= kScanEntries && p.n * p.entries <= kScanCompares;
     if (p.scan) {
