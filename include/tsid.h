@@ -612,7 +612,7 @@ tsid_status tsid_score_grad(tsid_ctx *ctx, const tsid_head *head, const int32_t 
                             const tsid_rows *dH, const tsid_rows *dF, void *ws, size_t ws_bytes, void *hip_stream);
 
 /* Distillation from a teacher's best items: row t lists n_ids items and the
- * teacher's logits of them.  With w_t the softmax of teacher_t / temperature
+ * teacher's logits of them (finite, or -inf for weight 0).  With w_t the softmax of teacher_t / temperature
  * over the listed items (without -1 and excluded ones),
  *   loss_t = temperature^2 sum_j w_tj (log w_tj - log p_t,ids[t, j]),
  * 0 for a row that lists none.  lse (not NULL) is kept for the gradient.

@@ -43,6 +43,7 @@ constexpr float kLeast = -1e8f;  // a running maximum before the first item
 typedef float f4 __attribute__((ext_vector_type(4)));
 typedef float f8 __attribute__((ext_vector_type(8)));
 typedef float f16 __attribute__((ext_vector_type(16)));
+typedef __bf16 b4 __attribute__((ext_vector_type(4)));
 typedef __bf16 b8 __attribute__((ext_vector_type(8)));
 typedef short s4 __attribute__((ext_vector_type(4)));
 
@@ -649,9 +650,10 @@ __device__ __forceinline__ float team_max(float v, double *red) {
 }
 
 // A row's results by one wave (TEAM 64), or by a workgroup where the best items
-// are wanted (256 threads; 512 for few rows, which leave the CUs to them: one row of
-// 1 M items 68 us instead of 73, with 1,024 threads 69, 257 rows 39, 40 and 53): the slices' sums joined in fp64, the given items' scores in fp64
-// (k / 8 lanes each), and the best items.  The best `top` items
+// are wanted (256 threads; 512 for few rows, which leave the CUs to them: one row
+// of 1 M items 68 us instead of 73, 257 rows of 17,770 39 instead of 40; 1,024
+// threads took 69 and 53): the slices' sums joined in fp64, the given items'
+// scores in fp64 (k / 8 lanes each), and the best items.  The best `top` items
 // lie in the `top` blocks of 32 whose maxima are largest (an item outside them
 // has `top` better ones), so those blocks and kMargin more, for the rounding of
 // the maxima, are scored again in fp64 and ranked by these scores.  The blocks
@@ -761,7 +763,7 @@ __global__ __launch_bounds__(TEAM == 64 ? kThreads : TEAM) void k_score_finish(F
         if (tm > -INFINITY) {
             listed([&](int j, int64_t, bool use, double z) {
                 const double lw = ((double)tl[j] - (double)tm) / A.tau, w = use ? exp(lw) : 0.0;
-                if (sub == 0 && w > 0.0) {
+                if (sub == 0 && w != 0.0) {  // a NaN logit reaches the loss
                     w_sum += w;
                     a_sum += w * (lw - (z - lse));
                 }
@@ -769,7 +771,7 @@ __global__ __launch_bounds__(TEAM == 64 ? kThreads : TEAM) void k_score_finish(F
         }
         w_sum = team_sum<TEAM>(w_sum, red);
         a_sum = team_sum<TEAM>(a_sum, red);
-        if (tid == 0) A.loss[t] = w_sum > 0.0 ? (float)(A.tau * A.tau * (a_sum / w_sum - log(w_sum))) : 0.f;
+        if (tid == 0) A.loss[t] = w_sum == 0.0 ? 0.f : (float)(A.tau * A.tau * (a_sum / w_sum - log(w_sum)));
     }
     if constexpr (TOP) {
         __shared__ uint64_t cand[kSelCap];
@@ -940,9 +942,14 @@ struct GradK {
     const int32_t *ids;
     const float *w;
     int32_t per_row;
+    // the items' gradient itself, where one slice holds all of it (else null)
+    void *out;
+    int64_t ldo;
+    float scale;
 };
 
-// Adds the listed items' part to a workgroup's sums of 128 items: of the
+// Ends a workgroup's sums of 128 items: adds the listed items' part, if it is
+// added here, and stores the sums, or where they are whole the gradient.  Of the
 // entries of its rows y (a slice), w h_y to the item that the entry lists.  The
 // sums go through LDS.  Entries are looked through 1,024 at a time (512 at k =
 // 128, where two workgroups share a CU's LDS); those of these items are listed
@@ -952,7 +959,7 @@ constexpr int listed_at_once(int K) { return K >= 128 ? 512 : 1024; }
 constexpr size_t listed_lds(int K) { return 128 * (size_t)K * 4 + (size_t)listed_at_once(K) * (12 + 8 * 2); }
 
 template <int K, int NP, int NB>
-__device__ __forceinline__ void add_listed(const GradK &A, const f16 (&acc)[NB], int64_t x0, int64_t i0, int64_t i1,
+__device__ __forceinline__ void finish_items(const GradK &A, const f16 (&acc)[NB], int64_t x0, int64_t i0, int64_t i1,
                                            int32_t slice, unsigned char *smem, uint32_t *wave_count) {
     constexpr int kListed = listed_at_once(K), P = kListed / kThreads;
     float *sum = reinterpret_cast<float *>(smem);  // [128][K]
@@ -1023,7 +1030,6 @@ __device__ __forceinline__ void add_listed(const GradK &A, const f16 (&acc)[NB],
                     m[q] = mine[team * kListed + std::min<uint32_t>(j + q, n_mine - 1)];
                     const int64_t from = (int64_t)row[m[q]] * A.Y.ld + c;
                     if constexpr (NP == 1) {
-                        typedef __bf16 b4 __attribute__((ext_vector_type(4)));
                         y[q] = __builtin_convertvector(
                             __builtin_bit_cast(b4, *reinterpret_cast<const uint2 *>(static_cast<const uint16_t *>(A.Y.p) + from)), f4);
                     } else {
@@ -1043,9 +1049,17 @@ __device__ __forceinline__ void add_listed(const GradK &A, const f16 (&acc)[NB],
     __syncthreads();
     for (int j = tid; j < 128 * K / 4; j += kThreads) {
         const int64_t x = x0 + j / (K / 4);
-        if (x < A.X.count)
-            *reinterpret_cast<f4 *>(A.part + ((int64_t)slice * A.X.count + x) * K + j % (K / 4) * 4) =
-                reinterpret_cast<const f4 *>(sum)[j];
+        if (x >= A.X.count) continue;
+        const f4 v = reinterpret_cast<const f4 *>(sum)[j];
+        const int at = j % (K / 4) * 4;
+        if (!A.out) {
+            *reinterpret_cast<f4 *>(A.part + ((int64_t)slice * A.X.count + x) * K + at) = v;
+        } else if constexpr (NP == 1) {
+            *reinterpret_cast<uint2 *>(static_cast<uint16_t *>(A.out) + x * A.ldo + at) =
+                __builtin_bit_cast(uint2, __builtin_convertvector(v * A.scale, b4));
+        } else {
+            *reinterpret_cast<f4 *>(static_cast<float *>(A.out) + x * A.ldo + at) = v * A.scale;
+        }
     }
 }
 
@@ -1194,8 +1208,8 @@ __device__ __forceinline__ void grad_pass(const GradK &A, int32_t block, unsigne
         }
     }
     if constexpr (ITEMS) {
-        if (A.per_row > 0) {
-            add_listed<K, NP>(A, acc, (int64_t)tile * 128, i0, i1, slice, smem, wave_count);
+        if (A.per_row > 0 || A.out) {
+            finish_items<K, NP>(A, acc, (int64_t)tile * 128, i0, i1, slice, smem, wave_count);
             return;
         }
     }
@@ -1374,7 +1388,7 @@ template <int K, int NP, bool ENT>
 void launch_grad(const GradK &rows, const GradK &items, hipStream_t s) {
     constexpr int YT = NP == 1 ? 64 : 32;
     constexpr size_t tiles = 3 * Tile<K, NP, YT>::kBytes, most = std::max(tiles, listed_lds(K));
-    const size_t lds = items.n_tiles && items.per_row > 0 ? most : tiles;
+    const size_t lds = items.n_tiles && (items.per_row > 0 || items.out) ? most : tiles;
     auto *pass = &k_grad_pass<K, NP, YT, ENT>;
     if (most > 64 * 1024) {
         static std::atomic<uint64_t> done;
@@ -1485,9 +1499,9 @@ GradPlan plan_grad(int64_t T, int64_t n, int k, int prec, int n_ids, Carve &c) {
     p.coef = c.take<float4>(T);
     p.w = c.take<float>(T * n_ids);
     p.h_part = c.take<float>((int64_t)p.h_slices * T * k);
-    p.f_part = c.take<float>((int64_t)p.f_slices * n * k);
     p.in_pass = T * n_ids > 0 && (int64_t)p.f_tiles * T * n_ids <= kInPass;
     p.sum.entries = p.in_pass ? 0 : T * n_ids;
+    p.f_part = c.take<float>(p.f_slices == 1 && p.sum.entries == 0 ? 0 : (int64_t)p.f_slices * n * k);
     p.sum.n = n;
     p.sum.k = k;
     carve_sum(p.sum, c);
@@ -1579,6 +1593,11 @@ void run_head_grad(const Head &h, const HeadGrad &g, void *ws, size_t bytes, int
             b.w = p.w;
             b.per_row = g.per_row;
         }
+        if (p.f_slices == 1 && p.sum.entries == 0) {  // one slice, and nothing to add: no sums in memory
+            b.out = g.dF.p;
+            b.ldo = g.dF.ld;
+            b.scale = (float)h.scale;
+        }
     }
     if (a.n_tiles || b.n_tiles)
         for_rank(h.k, h.prec, [&](auto kk, auto np) {
@@ -1595,7 +1614,7 @@ void run_head_grad(const Head &h, const HeadGrad &g, void *ws, size_t bytes, int
         });
         TSID_HIP(hipGetLastError());
     }
-    if (want_f) {
+    if (want_f && !b.out) {
         SumArgs sa{};
         sa.ids = g.ids;
         sa.bias = h.bias;
