@@ -39,6 +39,7 @@ constexpr int kThreads = 256;
 constexpr double kLog2e = 1.4426950408889634074, kLn2 = 0.69314718055994530942;
 constexpr float kOff = -1e9f;    // the exponent of an excluded item
 constexpr float kLeast = -1e8f;  // a running maximum before the first item
+constexpr float kPeak = -6.f;    // a gradient's exponent (log2 p) beyond which bf16 is too coarse for it
 
 typedef float f4 __attribute__((ext_vector_type(4)));
 typedef float f8 __attribute__((ext_vector_type(8)));
@@ -1068,9 +1069,15 @@ __device__ __forceinline__ void finish_items(const GradK &A, const f16 (&acc)[NB
 // alone is left to the sum's end).  The scores leave 16 rows of Y in a lane,
 // eight at a time the A operand of the second product (its k index counts rows
 // of Y in the order the scores left them); the B operand is a column of the
-// same rows of the tile, by transposing LDS reads (ds_read_b64_tr_b16).  g is
-// rounded to bf16 for bf16 factors (2^-9 of a term of a sum that is itself
-// rounded to bf16), and split in three parts for fp32 ones.
+// same rows of the tile, by transposing LDS reads (ds_read_b64_tr_b16).
+//
+// fp32 factors: g is split in three parts.  bf16: g is rounded to bf16, 2^-9 of a
+// term of a sum that is itself rounded to bf16 at the end.  But where a row is
+// nearly sure of its listed item the sum and the listed part cancel, and a
+// rounded p of 0.99 would be off by more than what is left; so a block of 32 x 32
+// with a p over 2^-6 adds the remainders in a second product (16 bits of g in
+// all).  The others' roundings then come to 2^-9 2^-3 of a row of F at most
+// (their squares add up to no more than 2^-6).
 template <int K, int NP, int YT, bool ITEMS, bool ENT>
 __device__ __forceinline__ void grad_pass(const GradK &A, int32_t block, unsigned char *smem, uint32_t *wave_count) {
     using S = Shape<K, NP>;
@@ -1132,8 +1139,10 @@ __device__ __forceinline__ void grad_pass(const GradK &A, int32_t block, unsigne
     auto start = [&](const uint16_t *b, int u) {
         return scores<K, NP, YT>(b + u * 32 * S::RS, x, NP == 1 ? per_row(offsets(b, u)) : f16{});
     };
-    // ... their g, in the parts that the second product takes
-    auto weights = [&](const f16 &s, const float *off, b8 (&ga)[2][NP]) {
+    // ... their g, in the parts that the second product takes, or (bf16, `rest`)
+    // what its rounding to bf16 leaves; returns the largest exponent
+    auto weights = [&](const f16 &s, const float *off, b8 (&ga)[2][NP], auto rest) {
+        float peak = kOff;
 #pragma unroll
         for (int h2 = 0; h2 < 2; ++h2) {
             f8 g;
@@ -1149,13 +1158,19 @@ __device__ __forceinline__ void grad_pass(const GradK &A, int32_t block, unsigne
                 for (int j = 0; j < 4; ++j) {
                     const float e = fmaf(s[4 * q + j], A.c, NP == 1 ? own_off : o[j] + own_off);
                     const float p = __builtin_amdgcn_exp2f(e);
+                    if constexpr (NP == 1) peak = fmaxf(peak, e);
                     if constexpr (ITEMS) g[4 * (q & 1) + j] = p * (ENT ? fmaf(e, yb[j], ya[j]) : ya[j]);
                     else g[4 * (q & 1) + j] = ENT ? p * fmaf(e, own_b, own_a) : p;
                 }
             }
-            if constexpr (NP == 1) ga[h2][0] = __builtin_convertvector(g, b8);
-            else split3(g, ga[h2]);
+            if constexpr (NP == 1) {
+                ga[h2][0] = __builtin_convertvector(g, b8);
+                if constexpr (rest()) ga[h2][0] = __builtin_convertvector(g - __builtin_convertvector(ga[h2][0], f8), b8);
+            } else {
+                split3(g, ga[h2]);
+            }
         }
+        return peak;
     };
     // acc += g times the 32 rows at yt
     auto products = [&](const uint16_t *yt, const b8 (&ga)[2][NP]) {
@@ -1197,8 +1212,12 @@ __device__ __forceinline__ void grad_pass(const GradK &A, int32_t block, unsigne
             for (int u = 0; u < YT / 32; ++u) {
                 b8 ga[2][NP];
                 const f16 next = start(u + 1 < YT / 32 ? buf(cur) : buf(nxt), u + 1 < YT / 32 ? u + 1 : 0);
-                weights(s, offsets(buf(cur), u), ga);
+                const float peak = weights(s, offsets(buf(cur), u), ga, std::false_type());
                 products(buf(cur) + u * 32 * S::RS, ga);
+                if (NP == 1 && __any(peak > kPeak)) {
+                    weights(s, offsets(buf(cur), u), ga, std::true_type());
+                    products(buf(cur) + u * 32 * S::RS, ga);
+                }
                 __builtin_amdgcn_sched_barrier(0);  // else reads of many blocks ahead spill
                 s = next;
             }

@@ -571,3 +571,37 @@ def test_refusals_of_the_library(X):
     assert grad(rows(F), None) == 1 and grad(None, rows(H)) == 1 and grad(None, None) == 0
     torch.cuda.synchronize()
     assert B.lib().tsid_lookup(X.ctx, 0, 16, None, None, C.c_float(1.0), None, None) == 1
+
+
+@pytest.mark.parametrize("prec", ["fp32", "bf16"])
+@pytest.mark.parametrize("T,n", [(7, 40), (150, 900)])
+def test_gradients_of_rows_that_are_sure(X, prec, T, n):
+    """Nearly all of a row's probability lies on the item that it lists, so that the dense and the listed part of
+    its gradient cancel to a few hundredths or less of each: what is left is as exact as the type.  bf16: a probability
+    up to 2^-6 is rounded (V), a larger one is carried to 2 V^2 (two parts); fp32 as elsewhere."""
+    g = np.random.default_rng(T)
+    k = 64
+    F, Fd = _table(g, n, k, prec)
+    ids = g.permutation(n)[:T].reshape(T, 1) if T <= n else g.integers(0, n, (T, 1))
+    H = F[_gpu(ids[:, 0], np.int64)].clone()
+    Hd = H.double().cpu().numpy()
+    scale = 0.2
+    note(f"rows that are sure {prec} T={T}")
+    dlogp = np.ones((T, 1), np.float32)
+    r = X.score(H, F, ids=_gpu(ids, np.int32), scale=scale)
+    assert float(r.logp.exp().median()) > 0.9
+    got = X.score_grad(H, F, r.lse, ids=_gpu(ids, np.int32), dlogp=_gpu(dlogp), scale=scale)
+    s = float(np.float32(scale))
+    dz, size = ref.dz_score(Hd, Fd, ids, dlogp, None, s, None)
+    none = np.zeros(n, bool)
+    z, lse, _, _ = ref.softmax_over(Hd, Fd, s, None, 1.0)
+    p, _ = ref.probabilities(z, lse)
+    zb = ref.z_bound(Hd, Fd, none, s, 1.0, None)
+    rel = (2 * zb + ref.lse_bound(zb, lse, n) + (8 + 2 * n + 2 * T) * ref.U)[:, None]
+    err = size * rel
+    if prec == "bf16":
+        # blocks of 32 x 32 decide together, so a probability may also be carried exactly where the bound rounds it
+        err = err + np.where(p <= 2.0 ** -6, ref.V, 2 * ref.V ** 2) * p
+    v = ref.V if prec == "bf16" else 2 * ref.U
+    for x, w, b, what in zip(got, ref.grads(dz, Hd, Fd, none, s), (s * err @ np.abs(Fd), s * err.T @ np.abs(Hd)), ("dH", "dF")):
+        _near(x, w, 1.01 * b + v * (np.abs(w) + b), what)
