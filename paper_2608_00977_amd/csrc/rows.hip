@@ -393,7 +393,7 @@ void check_workspace(const void *ws, size_t bytes, size_t needed) {
 }
 
 void carve_sum(SumPlan &p, Carve &c) {
-    p.scan = p.entries > 0 && p.entries <= kScanEntries && p.n * p.entries <= kScanCompares;
+    p.scan = p.entries > 0 && p.n > 0 && p.entries <= kScanEntries && p.n * p.entries <= kScanCompares;
     if (p.scan) {
         c.take<uint32_t>(1);  // a size of 0 says that the arguments are wrong
         return;
@@ -422,7 +422,7 @@ static void sum_sort(SumPlan &p, const int32_t *ids, const float *bias, int32_t 
 }
 
 void launch_sum_rows(SumPlan &p, int prec, const SumArgs &a, hipStream_t s) {
-    if (!p.scan || p.n <= 0) sum_sort(p, a.ids, a.bias, a.err, s);  // also reports ids of an empty table
+    if (!p.scan) sum_sort(p, a.ids, a.bias, a.err, s);  // reports the ids of an empty table too
     if (p.n <= 0) return;
     if (prec == TSID_BF16) sum_rows<uint16_t>(p, a, s);
     else sum_rows<float>(p, a, s);

@@ -605,3 +605,41 @@ def test_gradients_of_rows_that_are_sure(X, prec, T, n):
     v = ref.V if prec == "bf16" else 2 * ref.U
     for x, w, b, what in zip(got, ref.grads(dz, Hd, Fd, none, s), (s * err @ np.abs(Fd), s * err.T @ np.abs(Hd)), ("dH", "dF")):
         _near(x, w, 1.01 * b + v * (np.abs(w) + b), what)
+
+
+def test_gradient_into_an_empty_table(X):
+    import torch
+    import paper_2608_00977_amd as tsid
+    G = torch.ones((3, 8), device="cuda")
+    note("gradient into an empty table")
+    assert X.lookup_grad(G, _gpu([-1, -1, -1], np.int32), 0).shape == (0, 8)
+    X.rows_check()
+    X.lookup_grad(G, _gpu([-1, 0, -1], np.int32), 0)
+    with pytest.raises(tsid.TsidError) as e:
+        X.rows_check()
+    assert e.value.status == 2
+
+
+@pytest.mark.parametrize("prec", ["fp32", "bf16"])
+@pytest.mark.parametrize("T,n,m", [(40, 300, 0), (2, 5000, 3000), (100, 20000, 40), (2049, 130, 1)])
+def test_gradients_whatever_is_listed(X, prec, T, n, m):
+    """The entropy alone; long lists; lists on both sides of what is looked through in the pass, many of one item."""
+    k = 32
+    g, H, Hd, F, Fd, _, ids = _problem(T + m, T, n, k, prec, None, m)
+    if m > 1:
+        ids[:, 1:1 + m // 3] = np.where(g.random((T, m // 3)) < 0.5, 77, ids[:, 1:1 + m // 3])
+    none, scale = np.zeros(n, bool), 0.25
+    dlogp = g.standard_normal(ids.shape).astype(np.float32)
+    dent = g.standard_normal(T).astype(np.float32)
+    note(f"gradients {prec} T={T} n={n} listed={m}")
+    r = X.score(H, F, scale=scale, entropy=True)
+    listed = dict(ids=_gpu(ids, np.int32), dlogp=_gpu(dlogp)) if m else {}
+    got = X.score_grad(H, F, r.lse, entropy=r.entropy, dentropy=_gpu(dent), scale=scale, **listed)
+    dz, size = ref.dz_score(Hd, Fd, ids, dlogp, dent, scale, None)
+    # m more additions for a row, and up to T m for an item that all of them list
+    lse, zb = ref.softmax_over(Hd, Fd, scale, None, 1.0)[1], ref.z_bound(Hd, Fd, none, scale, 1.0, None)
+    for x, w, bound, what in zip(got, ref.grads(dz, Hd, Fd, none, scale),
+                                 ref.grad_bounds(size, Hd, Fd, none, scale, zb, lse, n + m, T * (m + 1), prec == "bf16"),
+                                 ("dH", "dF")):
+        _near(x, w, bound + (ref.V if prec == "bf16" else 2 * ref.U) * (np.abs(w) + bound), what)
+    X.rows_check()
