@@ -526,8 +526,8 @@ tsid_status tsid_get_timing(const tsid_ctx *ctx, tsid_timing *out);
  *    is not replayed after tsid_destroy.
  *  - ids are int32.  -1 stands for no item.  Another id outside the table is
  *    treated as -1 and reported as E_RANGE by the next tsid_rows_check.
- *  - Sums are fp32 or fp64 in a fixed order, without atomics: results repeat
- *    bit for bit.  Outputs must not overlap inputs or one another.
+ *  - Sums are fp32 or fp64 in a fixed order, without atomic additions: results
+ *    repeat bit for bit.  Outputs must not overlap inputs or one another.
  *  - Errors returned here: E_INVAL (NULL or misaligned pointer, bad size, k or
  *    option, workspace too small), E_DEVICE.  Empty sizes are allowed.
  */
@@ -549,10 +549,10 @@ tsid_status tsid_lookup(tsid_ctx *ctx, int32_t prec, int32_t k, const tsid_rows 
 
 /* Gradient of tsid_lookup in the table:
  *   dF[i] = scale * sum_(t: ids[t] = i) G[t]    for every row i of dF
- * (rows no id names get zeros).  The ids are sorted on the device (stable) and
- * each row of dF is summed in fp32 in the order of t (rows named more than 64
- * times: in pieces of the sorted list), rounded once and written once.
- * G->rows < 2^31. */
+ * (rows no id names get zeros).  The ids are sorted on the device (stable; few
+ * ids are looked through instead) and each row of dF is summed in fp32 in an
+ * order that the ids alone fix (rows named more than 64 times: in pieces of the
+ * sorted list), rounded once and written once.  G->rows < 2^31. */
 size_t tsid_lookup_grad_workspace(int64_t count, int64_t n, int32_t k);
 tsid_status tsid_lookup_grad(tsid_ctx *ctx, int32_t prec, int32_t k, const tsid_rows *G, const int32_t *ids,
                              float scale, const tsid_rows *dF, void *ws, size_t ws_bytes, void *hip_stream);
@@ -581,7 +581,7 @@ typedef struct {
 } tsid_head;
 
 /* Log probabilities of given items, with entropy and the best items.  Every
- * output may be NULL.
+ * output may be NULL (top_ids and top_logp with top = 0).
  *  ids      DEVICE T x n_ids or NULL (n_ids = 0): logp[t, j] = log p_t,ids[t, j],
  *           0 for id -1, -inf for an excluded item.
  *  lse      T: log sum_i exp z_ti.     entropy  T: -sum_i p_ti log p_ti.
@@ -612,8 +612,9 @@ tsid_status tsid_score_grad(tsid_ctx *ctx, const tsid_head *head, const int32_t 
                             const tsid_rows *dH, const tsid_rows *dF, void *ws, size_t ws_bytes, void *hip_stream);
 
 /* Distillation from a teacher's best items: row t lists n_ids items and the
- * teacher's logits of them (finite, or -inf for weight 0).  With w_t the softmax of teacher_t / temperature
- * over the listed items (without -1 and excluded ones),
+ * teacher's logits of them (finite, or -inf for weight 0).  With w_t the
+ * softmax of teacher_t / temperature over the listed items (without -1 and
+ * excluded ones),
  *   loss_t = temperature^2 sum_j w_tj (log w_tj - log p_t,ids[t, j]),
  * 0 for a row that lists none.  lse (not NULL) is kept for the gradient.
  * Workspace: tsid_score_workspace with top 0. */
