@@ -570,9 +570,9 @@ tsid_status tsid_lookup_grad(tsid_ctx *ctx, int32_t prec, int32_t k, const tsid_
  * excluded.
  * Scores of a row all of whose items are excluded (or n = 0): log sum -inf,
  * entropy 0, no best items, gradients 0.  A NaN in a row of H reaches that
- * row's results.  Products of bf16 factors are exact and added in fp32; fp32
- * factors are multiplied in three bf16 parts each, to about 2^-24 of the
- * product of the rows' norms. */
+ * row's results and dF, also of a row that lists no item.  Products of bf16
+ * factors are exact and added in fp32; fp32 factors are multiplied in three
+ * bf16 parts each, to about 2^-24 of the product of the rows' norms. */
 typedef struct {
     tsid_rows H, F;
     const float *bias;

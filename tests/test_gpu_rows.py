@@ -643,3 +643,36 @@ def test_gradients_whatever_is_listed(X, prec, T, n, m):
                                  ("dH", "dF")):
         _near(x, w, bound + (ref.V if prec == "bf16" else 2 * ref.U) * (np.abs(w) + bound), what)
     X.rows_check()
+
+
+@pytest.mark.parametrize("prec", ["fp32", "bf16"])
+@pytest.mark.parametrize("T", [3, 2100])
+def test_what_stands_beside_no_item_is_not_used(X, prec, T):
+    """Logits and weights at -1 and at excluded items: whatever they hold changes no bit."""
+    import torch
+    n, m = 70, 5
+    g = np.random.default_rng(T)
+    H, F = _table(g, T, 16, prec)[0], _table(g, n, 16, prec)[0]
+    bias = np.zeros(n, np.float32)
+    bias[::7] = -np.inf
+    ids = g.integers(0, n, (T, m)).astype(np.int32)
+    ids[:, 1] = -1
+    ids[:, 2] = 7  # excluded
+    ids[0] = -1
+    w = g.standard_normal((T, m)).astype(np.float32)
+    no_item = (ids < 0) | (ids % 7 == 0)
+    b, i = _gpu(bias), _gpu(ids, np.int32)
+    note(f"beside no item {prec} T={T}")
+    lse = X.score(H, F, bias=b).lse
+    first = None
+    for v in (0.0, np.nan, np.inf, -np.inf):
+        x = _gpu(np.where(no_item, np.float32(v), w))
+        loss, lse_d = X.distill(H, F, i, x, bias=b)
+        got = (loss, *X.distill_grad(H, F, i, x, lse_d, torch.ones_like(loss), bias=b),
+               *X.score_grad(H, F, lse, ids=i, dlogp=x, bias=b))
+        assert all(bool(torch.isfinite(o.float()).all()) for o in got), v
+        first = first or got
+        assert all(torch.equal(o, p) for o, p in zip(got, first)), v
+    H[0, 5] = float("nan")
+    dH, dF = X.score_grad(H, F, X.score(H, F, bias=b).lse, ids=i, dlogp=_gpu(np.where(no_item, np.float32(0), w)), bias=b)
+    assert bool(torch.isnan(dH[0]).any()) and bool(torch.isnan(dF).any()) and not bool(torch.isnan(dH[1:]).any())
