@@ -572,7 +572,9 @@ tsid_status tsid_lookup_grad(tsid_ctx *ctx, int32_t prec, int32_t k, const tsid_
  * entropy 0, no best items, gradients 0.  A NaN in a row of H reaches that
  * row's results and dF, also of a row that lists no item.  Products of bf16
  * factors are exact and added in fp32; fp32 factors are multiplied in three
- * bf16 parts each, to about 2^-24 of the product of the rows' norms. */
+ * bf16 parts each, to about 2^-24 of the product of the rows' norms.  The
+ * gradients' weights dz are multiplied in three bf16 parts too; with bf16
+ * factors in two (2^-16 of the weight) where the probability is at most 2^-6. */
 typedef struct {
     tsid_rows H, F;
     const float *bias;

@@ -39,7 +39,7 @@ constexpr int kThreads = 256;
 constexpr double kLog2e = 1.4426950408889634074, kLn2 = 0.69314718055994530942;
 constexpr float kOff = -1e9f;    // the exponent of an excluded item
 constexpr float kLeast = -1e8f;  // a running maximum before the first item
-constexpr float kPeak = -6.f;    // a gradient's exponent (log2 p) beyond which bf16 is too coarse for it
+constexpr float kPeak = -6.f;    // a gradient's exponent (log2 p) beyond which two bf16 parts are too coarse for it
 
 typedef float f4 __attribute__((ext_vector_type(4)));
 typedef float f8 __attribute__((ext_vector_type(8)));
@@ -1071,13 +1071,13 @@ __device__ __forceinline__ void finish_items(const GradK &A, const f16 (&acc)[NB
 // of Y in the order the scores left them); the B operand is a column of the
 // same rows of the tile, by transposing LDS reads (ds_read_b64_tr_b16).
 //
-// fp32 factors: g is split in three parts.  bf16: g is rounded to bf16, 2^-9 of a
-// term of a sum that is itself rounded to bf16 at the end.  But where a row is
-// nearly sure of its listed item the sum and the listed part cancel, and a
-// rounded p of 0.99 would be off by more than what is left; so a block of 32 x 32
-// with a p over 2^-6 adds the remainders in a second product (16 bits of g in
-// all).  The others' roundings then come to 2^-9 2^-3 of a row of F at most
-// (their squares add up to no more than 2^-6).
+// g is split as fp32 factors are: no product takes it in fewer bits than it has.
+// fp32 factors: three parts.  bf16: two, which leave 2^-16 of a term at most, and
+// a third in a product of its own in blocks of 32 x 32 with a p over 2^-6: what
+// is left out is then below 2^-22 of the row's weight whatever p is, as fp32's
+// own roundings are, also where the sum and the listed part nearly cancel (a row
+// sure of its item, equal rows of F).  The second part costs half as many matrix
+// products again, with the same reads of LDS.
 template <int K, int NP, int YT, bool ITEMS, bool ENT>
 __device__ __forceinline__ void grad_pass(const GradK &A, int32_t block, unsigned char *smem, uint32_t *wave_count) {
     using S = Shape<K, NP>;
@@ -1140,8 +1140,9 @@ __device__ __forceinline__ void grad_pass(const GradK &A, int32_t block, unsigne
         return scores<K, NP, YT>(b + u * 32 * S::RS, x, NP == 1 ? per_row(offsets(b, u)) : f16{});
     };
     // ... their g, in the parts that the second product takes, or (bf16, `rest`)
-    // what its rounding to bf16 leaves; returns the largest exponent
-    auto weights = [&](const f16 &s, const float *off, b8 (&ga)[2][NP], auto rest) {
+    // what those leave as the first of them; returns the largest exponent
+    constexpr int GP = NP == 1 ? 2 : NP;
+    auto weights = [&](const f16 &s, const float *off, b8 (&ga)[2][GP], auto rest) {
         float peak = kOff;
 #pragma unroll
         for (int h2 = 0; h2 < 2; ++h2) {
@@ -1165,15 +1166,17 @@ __device__ __forceinline__ void grad_pass(const GradK &A, int32_t block, unsigne
             }
             if constexpr (NP == 1) {
                 ga[h2][0] = __builtin_convertvector(g, b8);
-                if constexpr (rest()) ga[h2][0] = __builtin_convertvector(g - __builtin_convertvector(ga[h2][0], f8), b8);
+                g -= __builtin_convertvector(ga[h2][0], f8);
+                ga[h2][1] = __builtin_convertvector(g, b8);
+                if constexpr (rest()) ga[h2][0] = __builtin_convertvector(g - __builtin_convertvector(ga[h2][1], f8), b8);
             } else {
                 split3(g, ga[h2]);
             }
         }
         return peak;
     };
-    // acc += g times the 32 rows at yt
-    auto products = [&](const uint16_t *yt, const b8 (&ga)[2][NP]) {
+    // acc += g (rest: its first part) times the 32 rows at yt
+    auto products = [&](const uint16_t *yt, const b8 (&ga)[2][GP], auto rest) {
 #pragma unroll
         for (int h2 = 0; h2 < 2; ++h2) {
 #pragma unroll
@@ -1193,7 +1196,12 @@ __device__ __forceinline__ void grad_pass(const GradK &A, int32_t block, unsigne
                                                                    (__attribute__((address_space(3))) s4 *)(at + 8 * S::RS)));
                     yb[p] = __builtin_bit_cast(b8, make_uint4(lo.x, lo.y, hi.x, hi.y));
                 }
-                acc[nb] = product<NP>(ga[h2], yb, acc[nb]);
+                if constexpr (NP == 1) {
+                    if constexpr (!rest()) acc[nb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ga[h2][1], yb[0], acc[nb], 0, 0, 0);
+                    acc[nb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ga[h2][0], yb[0], acc[nb], 0, 0, 0);
+                } else {
+                    acc[nb] = product<NP>(ga[h2], yb, acc[nb]);
+                }
             }
         }
     };
@@ -1210,13 +1218,13 @@ __device__ __forceinline__ void grad_pass(const GradK &A, int32_t block, unsigne
             t.load(A.Y, y0 + 2 * YT);
 #pragma unroll
             for (int u = 0; u < YT / 32; ++u) {
-                b8 ga[2][NP];
+                b8 ga[2][GP];
                 const f16 next = start(u + 1 < YT / 32 ? buf(cur) : buf(nxt), u + 1 < YT / 32 ? u + 1 : 0);
                 const float peak = weights(s, offsets(buf(cur), u), ga, std::false_type());
-                products(buf(cur) + u * 32 * S::RS, ga);
+                products(buf(cur) + u * 32 * S::RS, ga, std::false_type());
                 if (NP == 1 && __any(peak > kPeak)) {
                     weights(s, offsets(buf(cur), u), ga, std::true_type());
-                    products(buf(cur) + u * 32 * S::RS, ga);
+                    products(buf(cur) + u * 32 * S::RS, ga, std::true_type());
                 }
                 __builtin_amdgcn_sched_barrier(0);  // else reads of many blocks ahead spill
                 s = next;
