@@ -1094,11 +1094,13 @@ __device__ __forceinline__ void grad_pass(const GradK &A, int32_t block, unsigne
     }
     b8 x[S::KS][NP];
     load_x<K, NP>(A.X, x0, A.turn, x);
-    // the lane's own part of the exponent's offset, and of the gradient
-    float own_off = 0.f, own_a = 0.f, own_b = 0.f;
+    // the lane's own part of the exponent's offset, and of the gradient; a row
+    // beyond the side has no probability (else its wave took it for a large one)
+    float own_off = kOff, own_a = 0.f, own_b = 0.f;
     if (xr < A.X.count) {
         if constexpr (ITEMS) {
-            if (A.X.bias) own_off = A.X.bias[xr] < kExcluded ? kOff : A.X.bias[xr] * A.bias_c;
+            own_off = A.X.bias ? A.X.bias[xr] : 0.f;
+            own_off = own_off < kExcluded ? kOff : own_off * A.bias_c;
         } else {
             const float4 q = A.coef[xr];
             own_off = -q.x;

@@ -92,3 +92,25 @@ def test_items_gradient_of_opposite_rows(X, prec, k, T, n):
     off = np.abs(dF.double().cpu().numpy() - want)
     bound = bound + (ref.V if prec == "bf16" else 2 * ref.U) * (np.abs(want) + bound)
     assert np.all(off <= bound), float((off / bound).max())
+
+
+@pytest.mark.parametrize("bias", [False, True])
+@pytest.mark.parametrize("k", [8, 64, 128])
+def test_rows_beside_none_take_the_same_products(X, k, bias):
+    """A row's gradient is the same bits whether the rows that share its wave are there or not: those beyond the last
+    one hold no large probability, for which a third part would be multiplied."""
+    import torch
+    g = np.random.default_rng(k)
+    n, T = 100, 128
+    F = _table(g, 1, k, "bf16")[0].expand(n, k).contiguous()  # equal items: all that is seen is what is left out
+    H, _ = _table(g, T, k, "bf16")
+    b = torch.full((n,), 3.0, device="cuda") if bias else None
+    ids, a = _gpu(g.integers(0, n, (T, 1)), np.int32), _gpu(g.standard_normal((T, 1)))
+    lse = X.score(H, F, scale=0.01, bias=b).lse
+    call = lambda t: X.score_grad(H[:t], F, lse[:t].contiguous(), ids=ids[:t].contiguous(), dlogp=a[:t].contiguous(),  # noqa: E731
+                                  scale=0.01, bias=b, want_F=False)[0]
+    note(f"rows beside none k={k} bias={bias}")
+    whole = call(T)
+    assert torch.count_nonzero(whole) > 0
+    for t in (1, 31, 33, 100, 127):
+        assert torch.equal(call(t), whole[:t]), t
