@@ -2,10 +2,10 @@
 // Scores (log sum, log probabilities of given items, entropy, best items),
 // distillation, and the gradients of both in H and F.
 //
-// No score ever reaches memory.  Both directions stream tiles of 32 rows of one
-// side (Y) past rows of the other side that stay in registers (X), one wave per
-// 32 or 64 of them, and take S = Y X^T with v_mfma_f32_32x32x16_bf16, which leaves
-// lane l with column l % 32 (its own row of X) and 16 of the 32 rows of Y (the
+// No score ever reaches memory.  Both directions stream tiles of one side (Y; 64
+// rows in bf16, 32 in fp32) past rows of the other side that stay in registers
+// (X), one wave per 32 or 64 of them, and take S = Y X^T, 32 rows of Y at a time,
+// with v_mfma_f32_32x32x16_bf16, which leaves lane l with column l % 32 (its own row of X) and 16 of the 32 rows of Y (the
 // matrix unit's rows 8 (r / 4) + 4 (l / 32) + r % 4, r = 0 .. 15): a row's running
 // maximum and sums are the lane's own, without any exchange.
 //
@@ -1386,9 +1386,12 @@ void allow_lds(const void *kernel, size_t lds, std::atomic<uint64_t> &done) {
 }
 
 // 64 rows per wave in bf16: two sets of products share each read of F's tile
-// (2,048 x 1 M, k = 128: 555 us; 32 rows: 647 us).  Tiles of 64 rows of F, but of
-// 32 where the blocks' maxima are kept, whose registers would spill otherwise
-// (880 and 992 us with the best 20).  fp32: 32 rows and tiles of 32, three parts each.
+// (2,048 x 1 M, k = 128: 555 us; 32 rows: 647 us).  Tiles of 64 rows of F, also
+// where the blocks' maxima are kept: at k = 128 a dozen registers spill then, and
+// still 2,048 x 1 M with entropy and the best 20 takes 920 us, in tiles of 32 rows,
+// which do not spill, 1,005 (k = 64: 630 and 730, k = 8: 512 and 570; 16,384 x
+// 100 k at k = 128 1,280 and 1,315, with a bias 1,487 and 1,432).  fp32: 32 rows and
+// tiles of 32, three parts each.
 template <int K, int NP, bool BIAS, bool ENT, bool TOP>
 void launch_score_pass(const ScoreK &a, hipStream_t s) {
     constexpr int CX = NP == 1 ? 2 : 1, YT = NP == 1 ? 64 : 32;
