@@ -566,15 +566,17 @@ tsid_status tsid_lookup_grad(tsid_ctx *ctx, int32_t prec, int32_t k, const tsid_
  *        and its row of F is not used, whatever it holds.  Otherwise finite.
  *  scale, temperature: scale / temperature is 0 or from 1e-12 to 1e12 in size,
  *        temperature from 1e-6 to 1e6.
- * Scores (divided by the temperature) lie above -5e7: lower ones count as
- * excluded.
- * Scores of a row all of whose items are excluded (or n = 0): log sum -inf,
- * entropy 0, no best items, gradients 0.  A NaN in a row of H reaches that
- * row's results and dF, also of a row that lists no item.  Products of bf16
- * factors are exact and added in fp32; fp32 factors are multiplied in three
- * bf16 parts each, to about 2^-24 of the product of the rows' norms.  The
- * gradients' weights dz are multiplied in three bf16 parts too; with bf16
- * factors in two (2^-16 of the weight) where the probability is at most 2^-6. */
+ * Scores (divided by the temperature) are fp32 sums and log sums are kept in
+ * fp32: probabilities are as exact as 2^-24 of a row's largest score allows.
+ * A row all of whose items are excluded, or have scores below -5e7 (or n = 0):
+ * log sum -inf, entropy 0, log probabilities -inf, loss 0, no best items,
+ * gradients 0.  (Items so far below others in their row just have p = 0.)
+ * A NaN in a row of H reaches that row's results and dF, also of a row that
+ * lists no item.  Products of bf16 factors are exact and added in fp32; fp32
+ * factors are multiplied in three bf16 parts each, to about 2^-24 of the
+ * product of the rows' norms.  The gradients' weights dz are multiplied in
+ * three bf16 parts too; with bf16 factors in two (2^-16 of the weight) where
+ * the probability is at most 2^-6. */
 typedef struct {
     tsid_rows H, F;
     const float *bias;

@@ -5,9 +5,10 @@
 // No score ever reaches memory.  Both directions stream tiles of one side (Y; 64
 // rows in bf16, 32 in fp32) past rows of the other side that stay in registers
 // (X), one wave per 32 or 64 of them, and take S = Y X^T, 32 rows of Y at a time,
-// with v_mfma_f32_32x32x16_bf16, which leaves lane l with column l % 32 (its own row of X) and 16 of the 32 rows of Y (the
-// matrix unit's rows 8 (r / 4) + 4 (l / 32) + r % 4, r = 0 .. 15): a row's running
-// maximum and sums are the lane's own, without any exchange.
+// with v_mfma_f32_32x32x16_bf16, which leaves lane l with column l % 32 (its own
+// row of X) and 16 of the 32 rows of Y (the matrix unit's rows 8 (r / 4) +
+// 4 (l / 32) + r % 4, r = 0 .. 15): a row's running maximum and sums are the
+// lane's own, without any exchange.
 //
 // fp32 factors are split into three bf16 parts each (8 + 8 + 8 bits, exact) and
 // multiplied part by part, six products for the nine (the other three are below
@@ -38,7 +39,10 @@ namespace {
 constexpr int kThreads = 256;
 constexpr double kLog2e = 1.4426950408889634074, kLn2 = 0.69314718055994530942;
 constexpr float kOff = -1e9f;    // the exponent of an excluded item
-constexpr float kLeast = -1e8f;  // a running maximum before the first item
+// A running maximum before the first item: -5e7 log2 e.  A row whose scores all
+// lie below is empty: its sum stays 0, and none of its items may be had, in the
+// results and in the gradients alike.
+constexpr float kLeast = -7.2134752e7f;
 constexpr float kPeak = -6.f;    // a gradient's exponent (log2 p) beyond which two bf16 parts are too coarse for it
 
 typedef float f4 __attribute__((ext_vector_type(4)));
@@ -690,7 +694,7 @@ __global__ __launch_bounds__(TEAM == 64 ? kThreads : TEAM) void k_score_finish(F
         if (A.lse) A.lse[t] = (float)lse;
         if (A.entropy) A.entropy[t] = empty ? 0.f : (float)(kLn2 * (log2(s) - e / s));
     }
-    auto usable = [&](int64_t id) { return id >= 0 && id < A.F.count && !(A.F.bias && A.F.bias[id] < kExcluded); };
+    auto usable = [&](int64_t id) { return !empty && id >= 0 && id < A.F.count && !(A.F.bias && A.F.bias[id] < kExcluded); };
     // the score of an item whose factors f the LN lanes hold
     auto score_of = [&](float bias, const f8 &f) {
         double z = 0.0;
@@ -736,7 +740,7 @@ __global__ __launch_bounds__(TEAM == 64 ? kThreads : TEAM) void k_score_finish(F
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 if (base + u * NI >= A.per_row) break;
-                const bool use = bias[u] >= kExcluded;
+                const bool use = !empty && bias[u] >= kExcluded;
                 const double z = score_of(use ? bias[u] : 0.f, eight(r[u]));
                 if (j0 + u * NI < A.per_row) visit(j0 + u * NI, id[u], use, z);
             }
@@ -847,7 +851,7 @@ __global__ __launch_bounds__(TEAM == 64 ? kThreads : TEAM) void k_score_finish(F
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 const int j = j0 + u * NI;
-                const bool use = bias[u] >= kExcluded;
+                const bool use = !empty && bias[u] >= kExcluded;
                 const double z = score_of(use ? bias[u] : 0.f, eight(r[u]));
                 if (sub == 0 && j < got * 32) cand[j] = use ? order_key(z) : 0ull;
             }

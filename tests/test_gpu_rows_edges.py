@@ -1,0 +1,112 @@
+"""The row operators at the ends of what they take: scores far from zero, the paths that sizes choose, signed
+zeros, what is refused."""
+import numpy as np
+import pytest
+
+import rows_ref as ref
+from gpu_util import note
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def X():
+    import paper_2608_00977_amd as tsid
+    t = tsid.Tsid(0)
+    yield t
+    t.close()
+
+
+def _gpu(a, dtype=np.float32):
+    import torch
+    return torch.from_numpy(np.ascontiguousarray(a, dtype)).cuda()
+
+
+def _table(g, rows, k, prec):
+    import torch
+    x = torch.from_numpy(g.standard_normal((rows, k)).astype(np.float32))
+    x = (x.bfloat16() if prec == "bf16" else x).cuda()
+    return x, x.double().cpu().numpy()
+
+
+# --------------------------------------------------- scores far from zero
+
+@pytest.mark.parametrize("prec", ["fp32", "bf16"])
+@pytest.mark.parametrize("T", [3, 45])
+def test_rows_far_below_zero_are_empty_in_results_and_gradients(X, prec, T):
+    """Scores of about -1e8: no item of the even rows may be had; the odd rows are ordinary."""
+    import torch
+    g = np.random.default_rng(T)
+    n, k, top = 70, 16, 4
+    F, Fd = _table(g, n, k, prec)
+    F[:, 0] = Fd[:, 0] = 1.0
+    H, Hd = _table(g, T, k, prec)
+    H[::2, 0] = -2.0 ** 27
+    H[1::2, 0] = 0.0
+    Hd = H.double().cpu().numpy()
+    ids = g.integers(0, n, (T, 2))
+    i, a = _gpu(ids, np.int32), _gpu(g.standard_normal((T, 2)))
+    note(f"rows far below zero {prec} T={T}")
+    r = X.score(H, F, ids=i, top=top, entropy=True)
+    even = slice(0, None, 2)
+    assert bool(torch.isneginf(r.lse[even]).all()) and bool(torch.isneginf(r.logp[even]).all())
+    assert bool(torch.isneginf(r.top_logp[even]).all()) and bool((r.top_ids[even] == -1).all())
+    assert torch.count_nonzero(r.entropy[even]) == 0
+    w = ref.score(Hd[1::2], Fd, ids[1::2], 1.0, None, top)
+    assert np.array_equal(r.top_ids[1::2].cpu().numpy(), w["top_ids"])
+    zb = ref.z_bound(Hd[1::2], Fd, np.zeros(n, bool), 1.0, 1.0, None)
+    assert np.all(np.abs(r.lse[1::2].double().cpu().numpy() - w["lse"]) <= ref.lse_bound(zb, w["lse"], n))
+    dH, dF = X.score_grad(H, F, r.lse, ids=i, dlogp=a, entropy=r.entropy, dentropy=torch.ones_like(r.lse))
+    assert torch.count_nonzero(dH[even]) == 0
+    odd = [x[1::2].contiguous() for x in (H, r.lse, i, a, r.entropy)]
+    _, want = X.score_grad(odd[0], F, odd[1], ids=odd[2], dlogp=odd[3], entropy=odd[4], dentropy=torch.ones_like(odd[1]))
+    size = ref.dz_score(Hd[1::2], Fd, ids[1::2], odd[3].cpu().numpy(), np.ones(len(odd[1])), 1.0, None)[1].T @ np.abs(Hd[1::2])
+    # the same terms, added in another order (T additions each) and rounded to the type
+    tol = size * (2 * (T + 2) * ref.U + (2 * ref.V if prec == "bf16" else 2 * ref.U))
+    assert np.all(np.abs((dF.double() - want.double()).cpu().numpy()) <= tol)
+    loss, lse = X.distill(H, F, i, a)
+    assert torch.count_nonzero(loss[even]) == 0 and bool(torch.isneginf(lse[even]).all())
+    dH, dF = X.distill_grad(H, F, i, a, lse, torch.ones_like(loss))
+    assert torch.count_nonzero(dH[even]) == 0 and bool(torch.isfinite(dF).all())
+
+
+@pytest.mark.parametrize("prec", ["fp32", "bf16"])
+def test_soft_masks_at_a_small_temperature(X, prec):
+    """A bias of -1e6 at temperature 0.01 on every item leaves nothing; on some, these have p = 0 and a finite log
+    probability, and the loss that lists them has the formula's gradient."""
+    import torch
+    g = np.random.default_rng(5)
+    T, n, k, m, tau = 40, 90, 32, 4, 0.01
+    F, Fd = _table(g, n, k, prec)
+    H, Hd = _table(g, T, k, prec)
+    ids = g.integers(0, n, (T, m))
+    teacher = (tau * g.standard_normal((T, m))).astype(np.float32)
+    dloss, scale = g.standard_normal(T).astype(np.float32), float(np.float32(0.002))
+    b = np.full(n, -1e6, np.float32)
+    i, t, d = _gpu(ids, np.int32), _gpu(teacher), _gpu(dloss)
+    note(f"soft masks {prec}")
+    opts = dict(scale=scale, temperature=tau, bias=_gpu(b))
+    loss, lse = X.distill(H, F, i, t, **opts)
+    assert bool(torch.isneginf(lse).all()) and torch.count_nonzero(loss) == 0
+    for x in X.distill_grad(H, F, i, t, lse, d, **opts):
+        assert torch.count_nonzero(x) == 0
+    far = np.arange(n) % 3 != 0
+    b[~far] = 0.0
+    opts["bias"] = _gpu(b)
+    loss, lse = X.distill(H, F, i, t, **opts)
+    want, wlse = ref.distill(Hd, Fd, ids, teacher, scale, b.astype(np.float64), tau)
+    zb = ref.z_bound(Hd, Fd, far, scale, tau, np.where(far, 0.0, b))  # of the items that have a probability
+    lb = ref.lse_bound(zb, wlse, n)
+    assert np.all(np.abs(lse.double().cpu().numpy() - wlse) <= lb)
+    assert np.all(np.abs(loss.double().cpu().numpy() - want) <= tau * tau * lb + 4 * ref.U * np.abs(want))
+    got = X.distill_grad(H, F, i, t, lse, d, **opts)
+    dz, size = ref.dz_distill(Hd, Fd, ids, teacher, dloss, scale, b.astype(np.float64), tau)
+    none, s = np.zeros(n, bool), scale / tau
+    bounds = ref.grad_bounds(size, Hd, Fd, none, s, zb, wlse, n, T, False)
+    # what two bf16 parts of a weight leave out
+    parts = (s * size @ np.abs(Fd), s * size.T @ np.abs(Hd))
+    v2, v = (ref.V ** 2, ref.V) if prec == "bf16" else (0.0, 2 * ref.U)
+    for x, w, bound, part in zip(got, ref.grads(dz, Hd, Fd, none, s), bounds, parts):
+        bound = bound + v2 * part
+        bound = bound + v * (np.abs(w) + bound)
+        assert np.all(np.abs(x.double().cpu().numpy() - w) <= bound)
