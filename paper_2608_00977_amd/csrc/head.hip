@@ -43,6 +43,7 @@ constexpr float kOff = -1e9f;    // the exponent of an excluded item
 // lie below is empty: its sum stays 0, and none of its items may be had, in the
 // results and in the gradients alike.
 constexpr float kLeast = -7.2134752e7f;
+constexpr float kNoRow = 1e25f;  // the log sum of a row that is none, or empty: p = 0 whatever is added to the exponent
 constexpr float kPeak = -6.f;    // a gradient's exponent (log2 p) beyond which two bf16 parts are too coarse for it
 
 typedef float f4 __attribute__((ext_vector_type(4)));
@@ -928,7 +929,7 @@ __global__ __launch_bounds__(kThreads) void k_head_coef(HeadGrad G, int64_t T, i
         const double l2 = (double)lse * kLog2e;
         const float l2f = (float)l2;
         const double d = (double)l2f - l2, f = exp2(d);  // log2 p = (c s - l2f) + d
-        coef[t] = empty ? make_float4(-kLeast, 0.f, 0.f, 0.f)
+        coef[t] = empty ? make_float4(kNoRow, 0.f, 0.f, 0.f)
                         : make_float4(l2f, (float)(f * (a + b * kLn2 * d)), (float)(f * b * kLn2), 0.f);
     }
 }
@@ -1121,7 +1122,7 @@ __device__ __forceinline__ void grad_pass(const GradK &A, int32_t block, unsigne
             const int64_t i = y0 + threadIdx.x;
             float *o = reinterpret_cast<float *>(b + NP * TL::kPlane) + offset_place(threadIdx.x);
             if constexpr (ITEMS) {
-                float4 q = make_float4(-kLeast, 0.f, 0.f, 0.f);
+                float4 q = make_float4(kNoRow, 0.f, 0.f, 0.f);
                 if (i < i1) q = A.coef[i];
                 o[0] = -q.x * A.unit;
                 o[YT] = q.y;

@@ -110,3 +110,21 @@ def test_soft_masks_at_a_small_temperature(X, prec):
         bound = bound + v2 * part
         bound = bound + v * (np.abs(w) + bound)
         assert np.all(np.abs(x.double().cpu().numpy() - w) <= bound)
+
+
+@pytest.mark.parametrize("prec", ["fp32", "bf16"])
+def test_scores_far_above_zero_leave_no_nan(X, prec):
+    """A bias of 250 at temperature 1e-6 (a score of 2.5e8) beside rows of a tile that are none."""
+    import torch
+    g = np.random.default_rng(9)
+    F, _ = _table(g, 40, 16, prec)
+    H = torch.zeros((3, 16), device="cuda").to(F.dtype)
+    b = np.zeros(40, np.float32)
+    b[5] = 250.0
+    ids = _gpu(np.full((3, 1), 5), np.int32)
+    t = torch.zeros((3, 1), device="cuda")
+    note(f"far above zero {prec}")
+    loss, lse = X.distill(H, F, ids, t, temperature=1e-6, scale=1e-6, bias=_gpu(b))
+    dH, dF = X.distill_grad(H, F, ids, t, lse, torch.ones_like(loss), temperature=1e-6, scale=1e-6, bias=_gpu(b))
+    for x in (loss, lse, dH, dF):
+        assert bool(torch.isfinite(x).all())
