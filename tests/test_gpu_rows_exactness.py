@@ -3,6 +3,7 @@ there is to see.  Bounds count roundings as rows_ref.py does (u = 2^-24; v = 2^-
 import numpy as np
 import pytest
 
+import rows_parts as parts
 import rows_ref as ref
 from gpu_util import note
 
@@ -114,3 +115,45 @@ def test_rows_beside_none_take_the_same_products(X, k, bias):
     assert torch.count_nonzero(whole) > 0
     for t in (1, 31, 33, 100, 127):
         assert torch.equal(call(t), whole[:t]), t
+
+
+# ------------------------------------- the products of three bf16 parts
+
+@pytest.mark.parametrize("many", [False, True])
+@pytest.mark.parametrize("k", [8, 16, 32, 64, 128])
+def test_scores_multiply_all_parts_of_fp32_factors(X, k, many):
+    """One item, and rows with one factor each: a log sum is one product of factors, nothing is added to it."""
+    import torch
+    x, y = parts.three_parts()
+    T = max(k, 40) if many else min(k, 32)
+    H = torch.zeros((T, k), device="cuda")
+    at = torch.arange(T, device="cuda")
+    H[at, (at + (k - 32 if k > 32 and not many else 0)) % k] = float(x)
+    F = torch.full((1, k), float(y), device="cuda")
+    note(f"products of parts k={k} many={many}")
+    for scale in (1.0, -1.0):
+        lse = X.score(H, F, scale=scale).lse.double().cpu().numpy()
+        # the six products, the exponent's constant, the exponential of what its rounding leaves (2 u), the result
+        bound = (parts.PARTS + 1 + 2 + 1) * ref.U * float(x) * float(y)
+        assert np.all(np.abs(lse - scale * float(x) * float(y)) <= bound)
+
+
+@pytest.mark.parametrize("k", [8, 16, 32, 64, 128])
+def test_gradients_multiply_all_parts_of_fp32_factors(X, k):
+    """Three items of equal scores, one listed, p = 1 / 3: a gradient's entries are one product of p and a factor."""
+    import torch
+    _, y = parts.three_parts()
+    rows = torch.full((1, k), float(y), device="cuda")
+    one = torch.ones((1, 1), device="cuda")
+    ids = torch.zeros((1, 1), dtype=torch.int32, device="cuda")
+    # p: the log sum's correction, the exponent and its exponential (1 u, 1 u, 2 u); the scale by a, the result
+    bound = (parts.PARTS + 4 + 2) * ref.U * float(y) / 3
+    note(f"products of parts, gradients k={k}")
+    F, H = torch.zeros((3, k), device="cuda"), torch.zeros((1, k), device="cuda")
+    F[2] = rows[0]  # dH = f_0 - (f_0 + f_1 + f_2) / 3
+    dH, _ = X.score_grad(H, F, X.score(H, F).lse, ids=ids, dlogp=one, want_F=False)
+    assert np.all(np.abs(dH.double().cpu().numpy() + float(y) / 3) <= bound)
+    F = torch.zeros((3, k), device="cuda")  # dF = (2 / 3, -1 / 3, -1 / 3) h
+    _, dF = X.score_grad(rows, F, X.score(rows, F).lse, ids=ids, dlogp=one, want_H=False)
+    want = np.array([2.0, -1.0, -1.0])[:, None] * float(y) / 3
+    assert np.all(np.abs(dF.double().cpu().numpy() - want) <= bound + 2 * ref.U * float(y))  # the sum with the listed part
