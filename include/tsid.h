@@ -543,7 +543,8 @@ typedef struct {
 tsid_status tsid_rows_check(tsid_ctx *ctx, void *hip_stream);
 
 /* out[t] = scale * F[ids[t]] for t < out->rows (embedding lookup with
- * scaling): the product in fp32, rounded once; zeros for id -1. */
+ * scaling): the product in fp32, rounded once; zeros for id -1.  scale is
+ * finite, here and in the gradient (E_INVAL). */
 tsid_status tsid_lookup(tsid_ctx *ctx, int32_t prec, int32_t k, const tsid_rows *F, const int32_t *ids, float scale,
                         const tsid_rows *out, void *hip_stream);
 

@@ -2762,6 +2762,11 @@ void check_rank_prec(int32_t k, int32_t prec) {
     if (prec != TSID_FP32 && prec != TSID_BF16) fail(TSID_E_INVAL, "bad precision");
 }
 
+// Not finite, it would make NaN of the zeros of rows that no id names.
+void check_scale(float scale) {
+    if (!std::isfinite(scale)) fail(TSID_E_INVAL, "scale must be finite");
+}
+
 Rows check_rows(const tsid_rows *r, int32_t k, int32_t prec, const char *what) {
     const std::string name(what);
     if (!r) fail(TSID_E_INVAL, name + " is NULL");
@@ -2782,7 +2787,7 @@ void check_array(const void *p, int64_t count, const char *what) {
 Head check_head(const tsid_head *h) {
     if (!h) fail(TSID_E_INVAL, "head is NULL");
     check_rank_prec(h->k, h->prec);
-    if (!std::isfinite(h->scale)) fail(TSID_E_INVAL, "scale must be finite");
+    check_scale(h->scale);
     if (!(h->temperature >= 1e-6f && h->temperature <= 1e6f)) fail(TSID_E_INVAL, "temperature must be in [1e-6, 1e6]");
     Head o{};
     o.H = check_rows(&h->H, h->k, h->prec, "H");
@@ -3048,6 +3053,7 @@ tsid_status tsid_lookup(tsid_ctx *c, int32_t prec, int32_t k, const tsid_rows *F
                         const tsid_rows *out, void *hip_stream) {
     return guarded_here(c, [&]() {
         check_rank_prec(k, prec);
+        check_scale(scale);
         const Rows f = check_rows(F, k, prec, "F"), o = check_rows(out, k, prec, "out");
         check_array(ids, o.count, "ids");
         launch_lookup(k, prec, f, ids, scale, o, c->rows_err, static_cast<hipStream_t>(hip_stream));
@@ -3069,6 +3075,7 @@ tsid_status tsid_lookup_grad(tsid_ctx *c, int32_t prec, int32_t k, const tsid_ro
                              float scale, const tsid_rows *dF, void *ws, size_t ws_bytes, void *hip_stream) {
     return guarded_here(c, [&]() {
         check_rank_prec(k, prec);
+        check_scale(scale);
         const Rows g = check_rows(G, k, prec, "G"), o = check_rows(dF, k, prec, "dF");
         check_array(ids, g.count, "ids");
         check_workspace(ws, ws_bytes, tsid_lookup_grad_workspace(g.count, o.count, k));

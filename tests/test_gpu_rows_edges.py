@@ -128,3 +128,20 @@ def test_scores_far_above_zero_leave_no_nan(X, prec):
     dH, dF = X.distill_grad(H, F, ids, t, lse, torch.ones_like(loss), temperature=1e-6, scale=1e-6, bias=_gpu(b))
     for x in (loss, lse, dH, dF):
         assert bool(torch.isfinite(x).all())
+
+
+# ----------------------------------------------------------------- refusals
+
+@pytest.mark.parametrize("scale", [float("nan"), float("inf"), -float("inf"), 1e39])
+def test_lookups_refuse_a_scale_that_is_not_finite(X, scale):
+    """Else the zeros of id -1 and of rows that no id names came out as NaN."""
+    import torch
+    import paper_2608_00977_amd as tsid
+    F, out = torch.ones((5, 8), device="cuda"), torch.full((2, 8), 7.0, device="cuda")
+    for call in (lambda: X.lookup(F, _gpu([1, -1], np.int32), scale=scale, out=out),
+                 lambda: X.lookup_grad(F[:2], _gpu([1, -1], np.int32), 2, scale=scale, out=out)):
+        with pytest.raises(tsid.TsidError) as e:
+            call()
+        assert e.value.status == 1
+    torch.cuda.synchronize()
+    assert bool((out == 7.0).all())
