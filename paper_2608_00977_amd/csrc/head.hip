@@ -516,15 +516,15 @@ constexpr int kSelCap = kMaxPick * 32;  // candidates chosen from at a time: the
 constexpr int kMaxGroups = 2048;        // one round of them
 static_assert(kMaxGroups <= kSelCap && kMaxPick <= 256, "");
 
-// Larger floats have larger keys; NaN is below everything.
+// Larger floats have larger keys, equal ones (both zeros) the same; NaN is below everything.
 __device__ __forceinline__ uint32_t order_key(float v) {
     if (!(v == v)) return 0u;
-    const uint32_t b = __float_as_uint(v);
+    const uint32_t b = __float_as_uint(v + 0.f);  // -0 + 0 = 0
     return (b & 0x80000000u) ? ~b : b | 0x80000000u;
 }
 __device__ __forceinline__ uint64_t order_key(double v) {
     if (!(v == v)) return 0ull;
-    const uint64_t b = __double_as_longlong(v);
+    const uint64_t b = __double_as_longlong(v + 0.0);
     return (b >> 63) ? ~b : b | (1ull << 63);
 }
 

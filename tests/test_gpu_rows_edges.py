@@ -145,3 +145,18 @@ def test_lookups_refuse_a_scale_that_is_not_finite(X, scale):
         assert e.value.status == 1
     torch.cuda.synchronize()
     assert bool((out == 7.0).all())
+
+
+@pytest.mark.parametrize("prec", ["fp32", "bf16"])
+@pytest.mark.parametrize("T", [3, 40])
+@pytest.mark.parametrize("scale", [1.0, -1.0, 0.0])
+def test_ties_of_zeros_of_both_signs_go_to_the_lowest_id(X, prec, T, scale):
+    """A zero row and a bias of 0 and -0: all scores are equal."""
+    import torch
+    g = np.random.default_rng(2)
+    F, _ = _table(g, 3000, 16, prec)
+    H = torch.zeros((T, 16), device="cuda").to(F.dtype)
+    bias = np.where(g.random(3000) < 0.5, -0.0, 0.0).astype(np.float32)
+    note(f"zeros of both signs {prec} T={T} scale={scale}")
+    r = X.score(H, F, scale=scale, bias=_gpu(bias), top=20)
+    assert r.top_ids.tolist() == [list(range(20))] * T
