@@ -881,7 +881,7 @@ __global__ __launch_bounds__(TEAM == 64 ? kThreads : TEAM) void k_score_finish(F
 // listed items.  One wave per row.
 __global__ __launch_bounds__(kThreads) void k_head_coef(HeadGrad G, int64_t T, int64_t n, const float *bias,
                                                         float4 *coef, float *w, int32_t *err) {
-    const int64_t t = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    const int64_t t = block_of_grid() * 4 + (threadIdx.x >> 6);
     if (t >= T) return;
     const int lane = threadIdx.x & 63;
     const int32_t *ids = G.ids ? G.ids + t * G.per_row : nullptr;
@@ -1264,8 +1264,9 @@ template <int K, int NP, int YT, bool ENT>
 __global__ __launch_bounds__(kThreads, 2) void k_grad_pass(GradK rows, GradK items, int32_t h_blocks) {
     extern __shared__ __align__(16) unsigned char smem[];
     __shared__ uint32_t wave_count[4];
-    if ((int32_t)blockIdx.x < h_blocks) grad_pass<K, NP, YT, false, ENT>(rows, blockIdx.x, smem, wave_count);
-    else grad_pass<K, NP, YT, true, ENT>(items, blockIdx.x - h_blocks, smem, wave_count);
+    const int64_t block = block_of_grid();  // below 2^26
+    if (block < h_blocks) grad_pass<K, NP, YT, false, ENT>(rows, (int32_t)block, smem, wave_count);
+    else if (items.n_tiles) grad_pass<K, NP, YT, true, ENT>(items, (int32_t)block - h_blocks, smem, wave_count);
 }
 
 // out[t] = scale (a_t * sum of the parts + sum_j w_tj F[id_tj]) (a_t in the
@@ -1276,7 +1277,7 @@ __global__ __launch_bounds__(kThreads) void k_grad_rows(const float *part, int32
                                                         int32_t per_row, const E *F, int64_t ldf, float scale, E *out,
                                                         int64_t ldo) {
     constexpr int LN = K / 8, U = 4;
-    const int64_t t = ((int64_t)blockIdx.x * kThreads + threadIdx.x) / LN;
+    const int64_t t = (block_of_grid() * kThreads + threadIdx.x) / LN;
     const int c = (int)(threadIdx.x % LN) * 8;
     if (t >= T) return;
     f8 sum = {}, more = {};
@@ -1348,14 +1349,17 @@ struct ScorePlan {
     float *blkmax, *sup;
 };
 
+// Rows of a run at most: 512 threads a row stay below the 2^32 of a launch.
+constexpr int64_t kRunRows = int64_t(1) << 22;
+
 ScorePlan plan_score(int64_t T, int64_t n, int prec, int top, Carve &c) {
     ScorePlan p{};
     p.nblk = (n + 63) / 64 * 2;
     p.few = T <= 32;
-    p.chunk = T;
-    if (top > 0) {  // at most 1 GiB of block maxima at a time
+    p.chunk = std::min(T, kRunRows);
+    if (top > 0) {  // at most 1 GiB of block maxima at a time, but of 256 rows at least (more from 33 M items on)
         const int64_t most = std::max<int64_t>(256, (int64_t(1) << 28) / std::max<int64_t>(p.nblk, 1) / 256 * 256);
-        p.chunk = std::min(T, most);
+        p.chunk = std::min(p.chunk, most);
     }
     p.cx = prec == TSID_BF16 ? 2 : 1;
     if (top > 0)
@@ -1433,7 +1437,7 @@ void launch_grad(const GradK &rows, const GradK &items, hipStream_t s) {
     }
     const int h_blocks = rows.n_tiles ? (grid_of(rows.n_slices, rows.n_tiles) + 7) / 8 * 8 : 0;
     const int f_blocks = items.n_tiles ? grid_of(items.n_slices, items.n_tiles) : 0;
-    pass<<<h_blocks + f_blocks, kThreads, lds, s>>>(rows, items, h_blocks);
+    pass<<<grid_of_blocks((int64_t)h_blocks + f_blocks), kThreads, lds, s>>>(rows, items, h_blocks);
     TSID_HIP(hipGetLastError());
 }
 
@@ -1600,7 +1604,7 @@ void run_head_grad(const Head &h, const HeadGrad &g, void *ws, size_t bytes, int
     check_workspace(ws, bytes, c.used);
     const bool ent = g.dentropy != nullptr;
     if (T > 0) {
-        k_head_coef<<<ceil_div(T, 4), kThreads, 0, s>>>(g, T, n, h.bias, p.coef, p.w, err);
+        k_head_coef<<<grid_of_blocks(ceil_div(T, 4)), kThreads, 0, s>>>(g, T, n, h.bias, p.coef, p.w, err);
         TSID_HIP(hipGetLastError());
     }
     GradK a{};
@@ -1645,7 +1649,7 @@ void run_head_grad(const Head &h, const HeadGrad &g, void *ws, size_t bytes, int
         const float4 *coef = ent ? nullptr : p.coef;
         for_rank(h.k, h.prec, [&](auto kk, auto np) {
             using E = std::conditional_t<np() == 1, uint16_t, float>;
-            k_grad_rows<E, kk()><<<ceil_div(T * (kk() / 8), kThreads), kThreads, 0, s>>>(
+            k_grad_rows<E, kk()><<<grid_of_blocks(ceil_div(T * (kk() / 8), kThreads)), kThreads, 0, s>>>(
                 p.h_part, p.h_slices, T, coef, g.ids, p.w, g.per_row, static_cast<const E *>(h.F.p), h.F.ld, (float)h.scale,
                 static_cast<E *>(g.dH.p), g.dH.ld);
         });

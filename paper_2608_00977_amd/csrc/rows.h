@@ -21,6 +21,14 @@ struct Carve {
     }
 };
 
+// A launch has fewer than 2^32 threads in x: more workgroups than kGridX (of at
+// most 512 threads) go on in y, whose last line has some beyond `blocks`.
+constexpr int64_t kGridX = int64_t(1) << 22;
+inline dim3 grid_of_blocks(int64_t blocks) {
+    return blocks <= kGridX ? dim3((unsigned)blocks) : dim3((unsigned)kGridX, (unsigned)((blocks + kGridX - 1) / kGridX));
+}
+__device__ __forceinline__ int64_t block_of_grid() { return (int64_t)blockIdx.y * gridDim.x + blockIdx.x; }
+
 // E_INVAL unless ws is 256-byte aligned and holds `needed` bytes (before any launch).
 void check_workspace(const void *ws, size_t bytes, size_t needed);
 

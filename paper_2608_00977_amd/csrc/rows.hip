@@ -55,8 +55,8 @@ template <typename E>
 __global__ __launch_bounds__(kThreads) void k_lookup(const E *F, int64_t n, int64_t ldf, const int32_t *ids,
                                                      int64_t count, float scale, E *out, int64_t ldo, int lanes_log,
                                                      int32_t *err) {
-    const int64_t g = ((int64_t)blockIdx.x * kThreads + threadIdx.x) >> lanes_log;
-    const int64_t groups = ((int64_t)gridDim.x * kThreads) >> lanes_log;
+    const int64_t g = (block_of_grid() * kThreads + threadIdx.x) >> lanes_log;
+    const int64_t groups = ((int64_t)gridDim.y * gridDim.x * kThreads) >> lanes_log;
     const int c = (threadIdx.x & ((1 << lanes_log) - 1)) * 8;
     bool bad = false;
     f8 v[kLookupRows];
@@ -216,7 +216,7 @@ __device__ __forceinline__ f8 sum_parts(const SumK &A, int64_t i, int c, int k) 
 template <int R, typename E>
 __global__ __launch_bounds__(kThreads) void k_sum_rows(SumK A, const E *X, E *out) {
     constexpr int U = R == 1 ? 0 : 2;  // entries loaded ahead
-    const int64_t i0 = (((int64_t)blockIdx.x * kThreads + threadIdx.x) >> A.lanes_log) * R;
+    const int64_t i0 = ((block_of_grid() * kThreads + threadIdx.x) >> A.lanes_log) * R;
     if (i0 >= A.n) return;
     const int c = (threadIdx.x & ((1 << A.lanes_log) - 1)) * 8, k = 8 << A.lanes_log;
     uint32_t at[R + 1];
@@ -272,7 +272,7 @@ __global__ __launch_bounds__(kThreads) void k_sum_rows(SumK A, const E *X, E *ou
 template <typename E>
 __global__ __launch_bounds__(kThreads) void k_sum_scan(SumK A, const int32_t *ids, const float *bias, const E *X,
                                                        E *out, int32_t *err) {
-    const int64_t i = (int64_t)blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6);
+    const int64_t i = block_of_grid() * (kThreads / 64) + (threadIdx.x >> 6);
     if (i >= A.n) return;
     const int lane = threadIdx.x & 63, lanes = 1 << A.lanes_log, groups = 64 >> A.lanes_log, grp = lane >> A.lanes_log;
     const int c = (lane & (lanes - 1)) * 8, k = 8 << A.lanes_log;
@@ -347,7 +347,7 @@ void sum_rows(const SumPlan &p, const SumArgs &a, hipStream_t s) {
     const E *X = static_cast<const E *>(a.X.p);
     E *out = static_cast<E *>(a.out.p);
     if (p.scan) {
-        k_sum_scan<E><<<ceil_div(p.n, kThreads / 64), kThreads, 0, s>>>(A, a.ids, a.bias, X, out, a.err);
+        k_sum_scan<E><<<grid_of_blocks(ceil_div(p.n, kThreads / 64)), kThreads, 0, s>>>(A, a.ids, a.bias, X, out, a.err);
         TSID_HIP(hipGetLastError());
         return;
     }
@@ -362,9 +362,9 @@ void sum_rows(const SumPlan &p, const SumArgs &a, hipStream_t s) {
         TSID_HIP(hipGetLastError());
     }
     if (p.entries * 4 <= p.n)
-        k_sum_rows<2, E><<<ceil_div((p.n + 1) / 2 << A.lanes_log, kThreads), kThreads, 0, s>>>(A, X, out);
+        k_sum_rows<2, E><<<grid_of_blocks(ceil_div((p.n + 1) / 2 << A.lanes_log, kThreads)), kThreads, 0, s>>>(A, X, out);
     else
-        k_sum_rows<1, E><<<ceil_div(p.n << A.lanes_log, kThreads), kThreads, 0, s>>>(A, X, out);
+        k_sum_rows<1, E><<<grid_of_blocks(ceil_div(p.n << A.lanes_log, kThreads)), kThreads, 0, s>>>(A, X, out);
     TSID_HIP(hipGetLastError());
 }
 
@@ -374,7 +374,7 @@ void launch_lookup(int k, int prec, const Rows &F, const int32_t *ids, float sca
                    hipStream_t s) {
     if (out.count <= 0) return;
     const int lg = lanes_log_of(k);
-    const int blocks = ceil_div(((out.count + kLookupRows - 1) / kLookupRows) << lg, kThreads);
+    const dim3 blocks = grid_of_blocks(ceil_div(((out.count + kLookupRows - 1) / kLookupRows) << lg, kThreads));
     if (prec == TSID_BF16)
         k_lookup<uint16_t><<<blocks, kThreads, 0, s>>>(static_cast<const uint16_t *>(F.p), F.count, F.ld, ids,
                                                        out.count, scale, static_cast<uint16_t *>(out.p), out.ld, lg,
