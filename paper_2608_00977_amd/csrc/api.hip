@@ -3066,6 +3066,7 @@ size_t tsid_lookup_grad_workspace(int64_t count, int64_t n, int32_t k) {
     p.entries = count;
     p.n = n;
     p.k = k;
+    p.plain = true;
     Carve carve;
     carve_sum(p, carve);
     return carve.used;
@@ -3083,6 +3084,7 @@ tsid_status tsid_lookup_grad(tsid_ctx *c, int32_t prec, int32_t k, const tsid_ro
         p.entries = g.count;
         p.n = o.count;
         p.k = k;
+        p.plain = true;
         Carve carve{static_cast<char *>(ws)};
         carve_sum(p, carve);
         hipStream_t s = static_cast<hipStream_t>(hip_stream);

@@ -49,6 +49,7 @@ void launch_lookup(int k, int prec, const Rows &F, const int32_t *ids, float sca
 struct SumPlan {
     int64_t entries, n;
     int k;
+    bool plain;          // a lookup's gradient: rows of X alone, without weights, exclusions and parts
     // pieces of the workspace
     uint64_t *keys[2];
     uint32_t *vals[2];
@@ -56,7 +57,7 @@ struct SumPlan {
     uint32_t *ptr;       // n + 1: first sorted entry of each row
     float *carry[2];     // sums of pieces of long rows, two per piece (two levels)
     bool alt;            // where the sort left its result
-    bool scan;           // few entries: no sort, none of these pieces
+    bool scan;           // few entries of a plain sum: no sort, none of these pieces
 };
 // Entries one piece of a long row's sum takes, and the row length from which
 // a row is summed in pieces.

@@ -265,32 +265,32 @@ __global__ __launch_bounds__(kThreads) void k_sum_rows(SumK A, const E *X, E *ou
     }
 }
 
-// The same sums without a sort: a wave per row of the table reads the ids of
+// A lookup's gradient without a sort: a wave per row of the table reads the ids of
 // all entries, 64 at a time, and its lane groups take the matching ones in
 // turn.  Few entries only: n times entries comparisons, and a row that all
 // entries name is one wave's work.
 template <typename E>
-__global__ __launch_bounds__(kThreads) void k_sum_scan(SumK A, const int32_t *ids, const float *bias, const E *X,
-                                                       E *out, int32_t *err) {
+__global__ __launch_bounds__(kThreads) void k_sum_scan(const int32_t *ids, int64_t entries, const E *X, int64_t ldx,
+                                                       float scale, E *out, int64_t n, int64_t ldo, int lanes_log,
+                                                       int32_t *err) {
     const int64_t i = block_of_grid() * (kThreads / 64) + (threadIdx.x >> 6);
-    if (i >= A.n) return;
-    const int lane = threadIdx.x & 63, lanes = 1 << A.lanes_log, groups = 64 >> A.lanes_log, grp = lane >> A.lanes_log;
-    const int c = (lane & (lanes - 1)) * 8, k = 8 << A.lanes_log;
-    const bool use = !(bias && bias[i] < kExcluded);
+    if (i >= n) return;
+    const int lane = threadIdx.x & 63, lanes = 1 << lanes_log, groups = 64 >> lanes_log, grp = lane >> lanes_log;
+    const int c = (lane & (lanes - 1)) * 8;
     f8 sum = f8{};
     bool bad = false;
     int turn = 0;  // of the groups
-    for (int64_t e0 = 0; e0 < A.entries; e0 += 256) {
+    for (int64_t e0 = 0; e0 < entries; e0 += 256) {
         int32_t id[4];
 #pragma unroll
         for (int x = 0; x < 4; ++x) {
             const int64_t e = e0 + 64 * x + lane;
-            id[x] = e < A.entries ? ids[e] : -1;
+            id[x] = e < entries ? ids[e] : -1;
         }
 #pragma unroll
         for (int x = 0; x < 4; ++x) {
-            bad |= id[x] < -1 || id[x] >= A.n;
-            uint64_t match = __ballot(use && id[x] == (int32_t)i);
+            bad |= id[x] < -1 || id[x] >= n;
+            uint64_t match = __ballot(id[x] == (int32_t)i);
             while (match) {  // `groups` matches at a time
                 uint32_t mine = ~0u;
                 for (int g = 0; g < groups && match; ++g) {
@@ -299,16 +299,13 @@ __global__ __launch_bounds__(kThreads) void k_sum_scan(SumK A, const int32_t *id
                     if (((turn + g) & (groups - 1)) == grp) mine = e;
                 }
                 turn += 1;
-                if (mine != ~0u) {
-                    const float w = A.w ? A.w[mine] : 1.f;
-                    sum += w * load8(X + (int64_t)source_row(A, mine) * A.ldx + c);
-                }
+                if (mine != ~0u) sum += load8(X + (int64_t)mine * ldx + c);
             }
         }
     }
     if (bad && i == 0) err[ERR_RANGE] = 1;
     for (int off = lanes; off < 64; off <<= 1) sum += other_lanes(sum, off);
-    if (grp == 0) store8(out + i * A.ldo + c, (sum + sum_parts(A, i, c, k)) * A.scale);
+    if (grp == 0) store8(out + i * ldo + c, sum * scale);
 }
 
 int lanes_log_of(int k) {
@@ -326,6 +323,14 @@ int64_t pieces_of(int64_t entries, int64_t span) { return (entries + span - 1) /
 
 template <typename E>
 void sum_rows(const SumPlan &p, const SumArgs &a, hipStream_t s) {
+    const E *X = static_cast<const E *>(a.X.p);
+    E *out = static_cast<E *>(a.out.p);
+    if (p.scan) {
+        k_sum_scan<E><<<grid_of_blocks(ceil_div(p.n, kThreads / 64)), kThreads, 0, s>>>(
+            a.ids, p.entries, X, a.X.ld, a.scale, out, p.n, a.out.ld, lanes_log_of(p.k), a.err);
+        TSID_HIP(hipGetLastError());
+        return;
+    }
     SumK A{};
     A.keys = p.keys[p.alt];
     A.vals = p.vals[p.alt];
@@ -344,13 +349,6 @@ void sum_rows(const SumPlan &p, const SumArgs &a, hipStream_t s) {
     A.part_stride = a.part_stride;
     A.scale = a.scale;
     A.ldo = a.out.ld;
-    const E *X = static_cast<const E *>(a.X.p);
-    E *out = static_cast<E *>(a.out.p);
-    if (p.scan) {
-        k_sum_scan<E><<<grid_of_blocks(ceil_div(p.n, kThreads / 64)), kThreads, 0, s>>>(A, a.ids, a.bias, X, out, a.err);
-        TSID_HIP(hipGetLastError());
-        return;
-    }
     if (p.entries > kSumPiece) {
         const int64_t n0 = pieces_of(p.entries, kSumPiece);
         k_sum_pieces<E, 0><<<ceil_div(n0 << (A.lanes_log + 2), kThreads), kThreads, 0, s>>>(A, X, n0);
@@ -393,7 +391,7 @@ void check_workspace(const void *ws, size_t bytes, size_t needed) {
 }
 
 void carve_sum(SumPlan &p, Carve &c) {
-    p.scan = p.entries > 0 && p.n > 0 && p.entries <= kScanEntries && p.n * p.entries <= kScanCompares;
+    p.scan = p.plain && p.entries > 0 && p.n > 0 && p.entries <= kScanEntries && p.n * p.entries <= kScanCompares;
     if (p.scan) {
         c.take<uint32_t>(1);  // a size of 0 says that the arguments are wrong
         return;
