@@ -62,10 +62,13 @@ struct SumPlan {
 // Entries one piece of a long row's sum takes, and the row length from which
 // a row is summed in pieces.
 constexpr int kSumPiece = 64;
-// Entries, and comparisons of ids, up to which every row looks through all
-// ids: 500 entries into 8,192 rows of 32 take 11 us in one launch, 34 with the
-// sort and the launches that follow it.
-constexpr int64_t kScanEntries = 2048, kScanCompares = int64_t(1) << 27;
+// Entries, and rows of the table, up to which every row looks through all ids
+// instead of a sort and the launches that follow it.  Entries of random ids, us
+// (looked through / sorted): 500 into 8,192 rows of 32 12 / 29, 2,048 12 / 33; at
+// the limits 2,048 into 65,536 rows of 128 47 / 48, of 8 53 / 41; beyond, 4,096
+// into 65,536 83 / 44, 1 into 1 M 331 / 32 (a wave per row).  A row that all
+// entries name is one wave's work: 500 entries 35 / 31, 2,048 133 / 35.
+constexpr int64_t kScanEntries = 2048, kScanRows = 65536;
 void carve_sum(SumPlan &p, Carve &c);
 // out[i] = scale * (sum of the entries of i + sum of the parts' rows i), every
 // row of out written; parts: n_parts fp32 arrays of n x k, part_stride apart.

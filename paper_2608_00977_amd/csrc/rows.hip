@@ -267,13 +267,12 @@ __global__ __launch_bounds__(kThreads) void k_sum_rows(SumK A, const E *X, E *ou
 
 // A lookup's gradient without a sort: a wave per row of the table reads the ids of
 // all entries, 64 at a time, and its lane groups take the matching ones in
-// turn.  Few entries only: n times entries comparisons, and a row that all
-// entries name is one wave's work.
+// turn.  Few entries and rows only (kScanEntries, kScanRows).
 template <typename E>
 __global__ __launch_bounds__(kThreads) void k_sum_scan(const int32_t *ids, int64_t entries, const E *X, int64_t ldx,
                                                        float scale, E *out, int64_t n, int64_t ldo, int lanes_log,
                                                        int32_t *err) {
-    const int64_t i = block_of_grid() * (kThreads / 64) + (threadIdx.x >> 6);
+    const int64_t i = (int64_t)blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6);
     if (i >= n) return;
     const int lane = threadIdx.x & 63, lanes = 1 << lanes_log, groups = 64 >> lanes_log, grp = lane >> lanes_log;
     const int c = (lane & (lanes - 1)) * 8;
@@ -326,7 +325,7 @@ void sum_rows(const SumPlan &p, const SumArgs &a, hipStream_t s) {
     const E *X = static_cast<const E *>(a.X.p);
     E *out = static_cast<E *>(a.out.p);
     if (p.scan) {
-        k_sum_scan<E><<<grid_of_blocks(ceil_div(p.n, kThreads / 64)), kThreads, 0, s>>>(
+        k_sum_scan<E><<<ceil_div(p.n, kThreads / 64), kThreads, 0, s>>>(
             a.ids, p.entries, X, a.X.ld, a.scale, out, p.n, a.out.ld, lanes_log_of(p.k), a.err);
         TSID_HIP(hipGetLastError());
         return;
@@ -391,7 +390,7 @@ void check_workspace(const void *ws, size_t bytes, size_t needed) {
 }
 
 void carve_sum(SumPlan &p, Carve &c) {
-    p.scan = p.plain && p.entries > 0 && p.n > 0 && p.entries <= kScanEntries && p.n * p.entries <= kScanCompares;
+    p.scan = p.plain && p.entries > 0 && p.n > 0 && p.entries <= kScanEntries && p.n <= kScanRows;
     if (p.scan) {
         c.take<uint32_t>(1);  // a size of 0 says that the arguments are wrong
         return;

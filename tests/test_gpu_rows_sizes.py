@@ -61,7 +61,6 @@ def test_gradients_of_more_than_2_26_rows(X):
 
 
 def test_lookup_gradient_into_more_than_2_26_rows(X):
-    """Few entries, which every row looks through."""
     import torch
     n = 2 ** 26 + 5
     G = torch.arange(1, 4, device="cuda").bfloat16()[:, None].expand(3, 8).contiguous()

@@ -1,0 +1,9 @@
+"""What the row operators choose by sizes, as the workspaces that they ask for show it (no GPU)."""
+from paper_2608_00977_amd import binding as B
+
+
+def test_a_lookup_gradient_is_summed_without_a_sort_into_small_tables_only():
+    for count, n in ((1, 1), (500, 8192), (2048, 65_536)):
+        assert B.tsid_lookup_grad_workspace(count, n, 32) == 256
+    for count, n in ((1, 1_000_000), (128, 100_000), (2049, 100)):  # keys and values twice, and a pointer per row
+        assert B.tsid_lookup_grad_workspace(count, n, 32) >= 24 * count + 4 * n
