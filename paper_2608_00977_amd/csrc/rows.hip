@@ -209,60 +209,29 @@ __device__ __forceinline__ f8 sum_parts(const SumK &A, int64_t i, int c, int k) 
     return sum;
 }
 
-// R neighbouring rows per lane group.  Two, with the first two entries of both
-// loaded ahead, where most rows have no entry (100 k rows of parts, 4,096 entries:
-// 23 us instead of 39); one where they have some: a wave waits for the longest of
-// its rows (1 M rows, 2 M entries: 169 us instead of 219).
-template <int R, typename E>
+// One row per lane group: a wave waits for the longest of its rows, so that two
+// rows each, with their first entries loaded ahead, are no faster where most rows
+// have no entry either (25 k entries into 100 k rows of 128: 58 us both ways).
+template <typename E>
 __global__ __launch_bounds__(kThreads) void k_sum_rows(SumK A, const E *X, E *out) {
-    constexpr int U = R == 1 ? 0 : 2;  // entries loaded ahead
-    const int64_t i0 = ((block_of_grid() * kThreads + threadIdx.x) >> A.lanes_log) * R;
-    if (i0 >= A.n) return;
+    const int64_t i = (block_of_grid() * kThreads + threadIdx.x) >> A.lanes_log;
+    if (i >= A.n) return;
     const int c = (threadIdx.x & ((1 << A.lanes_log) - 1)) * 8, k = 8 << A.lanes_log;
-    uint32_t at[R + 1];
-#pragma unroll
-    for (int r = 0; r <= R; ++r) at[r] = A.entries ? A.ptr[i0 + r < A.n ? i0 + r : A.n] : 0u;
-    f8 sum[R], v[R][U > 0 ? U : 1];
-    float w[R][U > 0 ? U : 1];
-#pragma unroll
-    for (int r = 0; r < R; ++r) {
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            v[r][u] = f8{};
-            w[r][u] = 0.f;
-            const uint32_t e = at[r] + u;
-            if (at[r + 1] - at[r] <= (uint32_t)kSumPiece && e < at[r + 1]) {
-                const uint32_t val = A.vals[e];
-                w[r][u] = A.w ? A.w[val] : 1.f;
-                v[r][u] = load8(X + (int64_t)source_row(A, val) * A.ldx + c);
-            }
-        }
-    }
-#pragma unroll
-    for (int r = 0; r < R; ++r) {
-        sum[r] = i0 + r < A.n ? sum_parts(A, i0 + r, c, k) : f8{};
-#pragma unroll
-        for (int u = 0; u < U; ++u)
-            if (w[r][u] != 0.f) sum[r] += w[r][u] * v[r][u];
-    }
-#pragma unroll
-    for (int r = 0; r < R; ++r) {
-        if (i0 + r >= A.n) break;
-        const uint32_t a = at[r], b = at[r + 1];
-        if (b - a > (uint32_t)kSumPiece) {
-            const bool two = A.two_levels && b - a > (uint32_t)(kSumPiece * kSumPiece);
-            const float *carry = two ? A.carry1 : A.carry0;
-            const int64_t span = two ? kSumPiece * kSumPiece : kSumPiece;
-            f8 more = f8{};
+    const uint32_t a = A.entries ? A.ptr[i] : 0u, b = A.entries ? A.ptr[i + 1] : 0u;
+    f8 sum = sum_parts(A, i, c, k);
+    if (b - a > (uint32_t)kSumPiece) {
+        const bool two = A.two_levels && b - a > (uint32_t)(kSumPiece * kSumPiece);
+        const float *carry = two ? A.carry1 : A.carry0;
+        const int64_t span = two ? kSumPiece * kSumPiece : kSumPiece;
+        f8 more = f8{};
 #pragma unroll 4
-            for (int64_t p = a / span; p < (b + span - 1) / span; ++p)
-                more += load8(carry + (p * 2 + (a > p * span ? 1 : 0)) * k + c);
-            sum[r] += more;
-        } else if (b - a > (uint32_t)U) {
-            sum[r] += sum_entries<4>(A, X, a + U, b, c);
-        }
-        store8(out + (i0 + r) * A.ldo + c, sum[r] * A.scale);
+        for (int64_t p = a / span; p < (b + span - 1) / span; ++p)
+            more += load8(carry + (p * 2 + (a > p * span ? 1 : 0)) * k + c);
+        sum += more;
+    } else if (b > a) {
+        sum += sum_entries<4>(A, X, a, b, c);
     }
+    store8(out + i * A.ldo + c, sum * A.scale);
 }
 
 // A lookup's gradient without a sort: a wave per row of the table reads the ids of
@@ -358,10 +327,7 @@ void sum_rows(const SumPlan &p, const SumArgs &a, hipStream_t s) {
         k_sum_pieces<E, 1><<<ceil_div(n1 << (A.lanes_log + 2), kThreads), kThreads, 0, s>>>(A, X, n1);
         TSID_HIP(hipGetLastError());
     }
-    if (p.entries * 4 <= p.n)
-        k_sum_rows<2, E><<<grid_of_blocks(ceil_div((p.n + 1) / 2 << A.lanes_log, kThreads)), kThreads, 0, s>>>(A, X, out);
-    else
-        k_sum_rows<1, E><<<grid_of_blocks(ceil_div(p.n << A.lanes_log, kThreads)), kThreads, 0, s>>>(A, X, out);
+    k_sum_rows<E><<<grid_of_blocks(ceil_div(p.n << A.lanes_log, kThreads)), kThreads, 0, s>>>(A, X, out);
     TSID_HIP(hipGetLastError());
 }
 

@@ -1,5 +1,5 @@
-"""The row operators' courses that sizes choose: listed items sorted beside the pass's parts, rows of a sum taken two
-at a time, sums of rows of every length."""
+"""The row operators' courses that sizes choose: listed items sorted beside the pass's parts, sums of rows of every
+length."""
 import numpy as np
 import pytest
 
@@ -36,7 +36,7 @@ def _near(got, want, bound, v, what):
 
 
 # More than 2^24 comparisons of ids by the workgroups of the items' pass (128 items each), so that the listed
-# items' part is sorted: 24 x 800,000 with rows of the sum one at a time, 782 x 25,000 with two at a time.
+# items' part is sorted: 24 x 800,000, 782 x 25,000.
 @pytest.mark.parametrize("prec", ["fp32", "bf16"])
 @pytest.mark.parametrize("T,n,m,k", [(2000, 3000, 400, 16), (250, 100_003, 100, 32)])
 def test_gradients_with_sorted_listed_items(X, prec, T, n, m, k):
@@ -90,7 +90,7 @@ def test_gradients_with_sorted_listed_items(X, prec, T, n, m, k):
 # Whole numbers, whose sums are exact in fp32, so that only the result is rounded.
 @pytest.mark.parametrize("prec", ["fp32", "bf16"])
 @pytest.mark.parametrize("k", [8, 32, 128])
-@pytest.mark.parametrize("n", [50_021, 100_000, 2_003])  # fewer than a quarter of the rows named (two at a time), and more
+@pytest.mark.parametrize("n", [50_021, 100_000, 2_003])  # few rows named, and many
 def test_lookup_gradient_of_rows_of_every_length(X, prec, k, n):
     import torch
     g = np.random.default_rng(n + k)
@@ -98,7 +98,7 @@ def test_lookup_gradient_of_rows_of_every_length(X, prec, k, n):
     rows = list(range(4, 4 + len(lengths) - 2)) + [n - 2, n - 1]  # beside one another, and the last two
     ids = np.concatenate([np.full(c, r) for r, c in zip(rows, lengths)] + [g.integers(100, n - 2, 600), np.full(37, -1)])
     ids = g.permutation(ids)
-    assert 2048 < len(ids) and (4 * len(ids) <= n) == (n != 2_003)
+    assert 2048 < len(ids)
     G = g.integers(-8, 9, (len(ids), k)).astype(np.float32)
     want = np.zeros((n, k))
     np.add.at(want, ids[ids >= 0], G[ids >= 0])
