@@ -1309,6 +1309,7 @@ __global__ __launch_bounds__(kThreads) void k_grad_rows(const float *part, int32
 // ------------------------------------------------------------- host side
 
 constexpr int kCus = 256;
+constexpr int64_t kSlots = 2 * kCus;  // workgroups of a pass at a time
 
 // How a streamed side of `rows` rows is cut: `tiles` workgroups per slice, of
 // which two fit a CU; slices of whole units, a multiple of the 8 XCDs from 8
@@ -1319,7 +1320,6 @@ void slices_of(int64_t rows, int64_t tiles, int64_t unit, double slice_cost, int
     double best = 0.0;
     n_slices = 1;
     slice_rows = unit;
-    constexpr int64_t kSlots = 2 * kCus;
     tiles = std::max<int64_t>(1, tiles);  // an empty side
     auto look = [&](int64_t ns) {
         if (ns >= 8) ns = ns / 8 * 8;
@@ -1521,11 +1521,14 @@ struct GradPlan {
     SumPlan sum;
 };
 
-// Ids that all workgroups of the items' gradient together look through at most
-// for the listed items' part; beyond, the entries are sorted, which costs seven
-// more launches.  4,096 rows with 20 listed of 8,192 items (5.2 M looked at): 199
-// us in the pass, 230 with the sort; 611 rows, 18 of 16,733 items: 81 and 118;
-// 16,384 rows, 50 of 100 k items (640 M) stay with the sort.
+// Ids that the workgroups of the items' gradient look through at most for the
+// listed items' part, all slots of the device together, taken or not (with few
+// workgroups each looks through more); beyond, the entries are sorted, which
+// costs seven more launches.  dF in the pass / with the sort, us: 4,096 rows, 20
+// listed of 8,192 items (5.2 M) 90 / 112, 50 listed (13 M) 125 / 124, 100 listed
+// (26 M) 180 / 147; 2,048 rows, 10 listed of 100 k (16 M) 266 / 260; 256 rows, 8
+// listed of 1 M (16 M) 216 / 277; 1,000 rows, 100 listed of 20 k (17 M, 157
+// workgroups a slice) 96 / 70; 512 rows, 1,000 listed of 2,000 (33 M, 16) 241 / 99.
 constexpr int64_t kInPass = int64_t(1) << 24;
 
 GradPlan plan_grad(int64_t T, int64_t n, int k, int prec, int n_ids, Carve &c) {
@@ -1540,8 +1543,9 @@ GradPlan plan_grad(int64_t T, int64_t n, int k, int prec, int n_ids, Carve &c) {
     p.coef = c.take<float4>(T);
     p.w = c.take<float>(T * n_ids);
     p.h_part = c.take<float>((int64_t)p.h_slices * T * k);
-    p.in_pass = T * n_ids > 0 && (int64_t)p.f_tiles * T * n_ids <= kInPass;
-    p.sum.entries = p.in_pass ? 0 : T * n_ids;
+    const int64_t listed = T * n_ids;
+    p.in_pass = listed > 0 && std::max(p.f_tiles * listed, kSlots * ((listed + p.f_slices - 1) / p.f_slices)) <= kInPass;
+    p.sum.entries = p.in_pass ? 0 : listed;
     p.f_part = c.take<float>(p.f_slices == 1 && p.sum.entries == 0 ? 0 : (int64_t)p.f_slices * n * k);
     p.sum.n = n;
     p.sum.k = k;
