@@ -160,3 +160,80 @@ def test_ties_of_zeros_of_both_signs_go_to_the_lowest_id(X, prec, T, scale):
     note(f"zeros of both signs {prec} T={T} scale={scale}")
     r = X.score(H, F, scale=scale, bias=_gpu(bias), top=20)
     assert r.top_ids.tolist() == [list(range(20))] * T
+
+
+# ------------------------------------------------- the C entry points' forms
+
+def _c(X):
+    """The library, and tables as its structures."""
+    from paper_2608_00977_amd import binding as B
+    return B, lambda x: B.tsid_rows(x.data_ptr(), x.shape[0], x.stride(0))
+
+
+def _ws(nbytes):
+    import torch
+    ws = torch.empty(nbytes + 256, dtype=torch.uint8, device="cuda")
+    return ws, (ws.data_ptr() + 255) & ~255
+
+
+@pytest.mark.parametrize("prec", ["fp32", "bf16"])
+@pytest.mark.parametrize("T", [9, 70])
+def test_scores_at_a_temperature_and_any_output_alone(X, prec, T):
+    """tsid_score divides by the head's temperature as a scale and a bias that are divided by it do (a power of two,
+    so the same bits), and gives the same where only some outputs are wanted."""
+    import torch
+    B, rows = _c(X)
+    g = np.random.default_rng(T)
+    n, k, top = 333, 32, 6
+    F, _ = _table(g, n, k, prec)
+    H, _ = _table(g, T, k, prec)
+    bias, ids = _gpu(g.standard_normal(n)), _gpu(g.integers(-1, n, (T, 3)), np.int32)
+    want = X.score(H, F, ids=ids, scale=0.25, bias=bias / 4, top=top, entropy=True)
+    head = B.tsid_head(rows(H), rows(F), bias.data_ptr(), k, B.BF16 if prec == "bf16" else B.FP32, 1.0, 4.0)
+    outs = [torch.empty_like(x) for x in want]  # lse, logp, entropy, top_ids, top_logp
+    note(f"temperature {prec} T={T}")
+    for wanted in ((0, 1, 2, 3, 4), (0,), (1,), (2,), (3, 4), ()):
+        for o in outs:
+            o.fill_(77)
+        t = top if 3 in wanted else 0
+        need = B.tsid_score_workspace(T, n, k, head.prec, t)
+        ws, at = _ws(need)
+        p = [o.data_ptr() if q in wanted else None for q, o in enumerate(outs)]
+        st = B.tsid_score(X.ctx, head, ids.data_ptr() if 1 in wanted else None, 3 if 1 in wanted else 0, t, p[0], p[1], p[2],
+                          p[3], p[4], at, need, torch.cuda.current_stream().cuda_stream)
+        assert st == 0
+        torch.cuda.synchronize()
+        for q, (o, w) in enumerate(zip(outs, want)):
+            assert torch.equal(o, w) if q in wanted else bool((o == 77).all()), (wanted, q)
+    # the gradient at a temperature
+    a = _gpu(g.standard_normal((T, 3)))
+    w = X.score_grad(H, F, want.lse, ids=ids, dlogp=a, scale=0.25, bias=bias / 4)
+    need = B.tsid_head_grad_workspace(T, n, k, head.prec, 3)
+    ws, at = _ws(need)
+    full = [torch.full((x.shape[0] + 2, k + 16), 5.0, device="cuda").to(x.dtype) for x in (H, F)]
+    views = [f[1:-1, 8:8 + k] for f in full]
+    st = B.tsid_score_grad(X.ctx, head, ids.data_ptr(), 3, want.lse.data_ptr(), a.data_ptr(), None, None, rows(views[0]),
+                           rows(views[1]), at, need, torch.cuda.current_stream().cuda_stream)
+    assert st == 0
+    torch.cuda.synchronize()
+    for f, v, x in zip(full, views, w):
+        assert torch.equal(v, x)
+        v.fill_(5.0)
+        assert bool((f == 5.0).all())  # what lies beside the strided rows is as it was
+
+
+def test_an_error_is_reported_once_whichever_stream_met_it(X):
+    import torch
+    import paper_2608_00977_amd as tsid
+    F = torch.ones((4, 8), device="cuda")
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        X.lookup(F, _gpu([9], np.int32))
+    side.synchronize()
+    with pytest.raises(tsid.TsidError) as e:
+        X.rows_check()
+    assert e.value.status == 2
+    X.rows_check()
+    with torch.cuda.stream(side):
+        X.rows_check()
