@@ -287,7 +287,7 @@ struct tsid_ctx {
     int32_t row_blocks = 0;           // tsid_set_row_blocks: 0 automatic, 1 off, n forced
     int32_t used_blocks = 1;          // row blocks of the last fit's Q pass
     void *noalloc_scratch = nullptr;  // device address of this device's scratch array
-    int32_t *rows_err = nullptr;      // error slots of the row operators
+    int32_t *rows_err = nullptr;      // error slots of the row operators, and what a check took from them
 };
 
 namespace {
@@ -2826,13 +2826,12 @@ void rows_check(tsid_ctx *c, hipStream_t s) {
     hipStreamCaptureStatus cap = hipStreamCaptureStatusNone;
     TSID_HIP(hipStreamIsCapturing(s, &cap));
     if (cap != hipStreamCaptureStatusNone) fail(TSID_E_STATE, "the stream is being captured");
+    // read and cleared in one step: what another stream's call reports meanwhile is kept for the next check
     int32_t e[ERR_SLOTS];
-    TSID_HIP(hipMemcpyAsync(e, c->rows_err, sizeof(e), hipMemcpyDeviceToHost, s));
+    launch_take_slots(c->rows_err, c->rows_err + ERR_SLOTS, ERR_SLOTS, s);
+    TSID_HIP(hipMemcpyAsync(e, c->rows_err + ERR_SLOTS, sizeof(e), hipMemcpyDeviceToHost, s));
     TSID_HIP(hipStreamSynchronize(s));
-    if (!e[ERR_RANGE]) return;
-    fill_i32(c->rows_err, ERR_SLOTS, 0, s);
-    TSID_HIP(hipStreamSynchronize(s));
-    fail(TSID_E_RANGE, "row operators: id out of range");
+    if (e[ERR_RANGE]) fail(TSID_E_RANGE, "row operators: id out of range");
 }
 
 }  // namespace
@@ -2864,8 +2863,8 @@ tsid_status tsid_create(int device, void *hip_stream, size_t max_device_bytes, t
         c->err_dev = c->arena.alloc<int32_t>(ERR_SLOTS);
         TSID_HIP(hipHostMalloc((void **)&c->err_host, ERR_SLOTS * sizeof(int32_t), hipHostMallocDefault));
         TSID_HIP(hipMemset(c->err_dev, 0, ERR_SLOTS * sizeof(int32_t)));
-        c->rows_err = c->arena.alloc<int32_t>(ERR_SLOTS);
-        TSID_HIP(hipMemset(c->rows_err, 0, ERR_SLOTS * sizeof(int32_t)));
+        c->rows_err = c->arena.alloc<int32_t>(2 * ERR_SLOTS);
+        TSID_HIP(hipMemset(c->rows_err, 0, 2 * ERR_SLOTS * sizeof(int32_t)));
         c->noalloc_scratch = noalloc_scratch_on(device);
     });
     if (st != TSID_OK) {

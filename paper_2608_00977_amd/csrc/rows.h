@@ -32,6 +32,9 @@ __device__ __forceinline__ int64_t block_of_grid() { return (int64_t)blockIdx.y 
 // E_INVAL unless ws is 256-byte aligned and holds `needed` bytes (before any launch).
 void check_workspace(const void *ws, size_t bytes, size_t needed);
 
+// taken[j] = slots[j], and slots[j] = 0, for j < n (at most 64), each in one step.
+void launch_take_slots(int32_t *slots, int32_t *taken, int n, hipStream_t s);
+
 // Rows of a factor table: fp32 or bf16, k per row, ld elements from row to row.
 struct Rows {
     void *p;

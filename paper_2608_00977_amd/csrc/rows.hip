@@ -77,6 +77,10 @@ __global__ __launch_bounds__(kThreads) void k_lookup(const E *F, int64_t n, int6
     if (bad) err[ERR_RANGE] = 1;
 }
 
+__global__ void k_take_slots(int32_t *slots, int32_t *taken, int n) {
+    if ((int)threadIdx.x < n) taken[threadIdx.x] = atomicExch(slots + threadIdx.x, 0);
+}
+
 // key = id (n for an entry that adds nothing), value = entry.
 __global__ __launch_bounds__(kThreads) void k_sum_keys(const int32_t *ids, int64_t entries, int64_t n,
                                                        const float *bias, uint64_t *keys, uint32_t *vals,
@@ -345,6 +349,11 @@ void launch_lookup(int k, int prec, const Rows &F, const int32_t *ids, float sca
     else
         k_lookup<float><<<blocks, kThreads, 0, s>>>(static_cast<const float *>(F.p), F.count, F.ld, ids, out.count,
                                                     scale, static_cast<float *>(out.p), out.ld, lg, err);
+    TSID_HIP(hipGetLastError());
+}
+
+void launch_take_slots(int32_t *slots, int32_t *taken, int n, hipStream_t s) {
+    k_take_slots<<<1, 64, 0, s>>>(slots, taken, n);
     TSID_HIP(hipGetLastError());
 }
 
