@@ -546,7 +546,8 @@ class Tsid:
     # outputs and scratch come from torch's allocator (so they may be captured
     # into a graph, and calls on several streams share nothing).  Factor tables
     # are fp32 or bf16 tensors of k = 8, 16, 32, 64 or 128 columns, rows of any
-    # 16-byte aligned stride.
+    # 16-byte aligned stride.  Gradients are calls of their own: results carry no
+    # autograd history, whether or not their inputs require gradients.
 
     def _stream(self) -> int:
         # the handle alone: torch.cuda.current_stream() makes a Stream object of it first (2.5 us of a 10 us call)
@@ -615,7 +616,8 @@ class Tsid:
 
     def lookup(self, F: torch.Tensor, ids: torch.Tensor, scale: float = 1.0,
                out: Optional[torch.Tensor] = None) -> torch.Tensor:
-        """Rows of F by id, scaled; zeros for id -1 (tsid_lookup)."""
+        """Rows of F by id, scaled; zeros for id -1 (tsid_lookup).  Its gradient
+        is lookup_grad; the result has no autograd history."""
         f = self._rows("F", F)
         self._on_device("ids", ids, torch.int32)
         if out is None:
@@ -650,7 +652,8 @@ class Tsid:
     def score(self, H: torch.Tensor, F: torch.Tensor, ids: Optional[torch.Tensor] = None, scale: float = 1.0,
               bias: Optional[torch.Tensor] = None, top: int = 0, entropy: bool = False) -> Scores:
         """Log sums, log probabilities of the items `ids` (T x m), entropy and
-        the `top` best items of every row of H over all rows of F (tsid_score)."""
+        the `top` best items of every row of H over all rows of F (tsid_score).
+        Their gradient is score_grad; the results have no autograd history."""
         head = self._head(H, F, scale, bias)
         m, T, top = self._listed(H, ids), H.shape[0], int(top)
         r = Scores(self._new(T), self._new((T, m)) if ids is not None else None, self._new(T) if entropy else None,
@@ -690,7 +693,8 @@ class Tsid:
     def distill(self, H: torch.Tensor, F: torch.Tensor, ids: torch.Tensor, teacher: torch.Tensor,
                 scale: float = 1.0, temperature: float = 1.0, bias: Optional[torch.Tensor] = None):
         """(loss, lse) per row of H: the divergence from a teacher's logits of
-        the items `ids` (both T x m) to the factors' probabilities (tsid_distill)."""
+        the items `ids` (both T x m) to the factors' probabilities (tsid_distill).
+        Its gradient is distill_grad; the results have no autograd history."""
         head = self._head(H, F, scale, bias, temperature)
         m = self._listed(H, ids, ("teacher", teacher))
         loss, lse = self._new(H.shape[0]), self._new(H.shape[0])

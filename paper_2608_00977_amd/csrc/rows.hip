@@ -17,8 +17,8 @@
 //
 // Measured (one MI355X): 1,000,003 rows of 128 fp32 by popular ids in 188 us, 5.4
 // TB/s of the 1.02 GB that no repeated row is counted in (a copy moves 4.7).  2 M
-// bf16 rows of 128 into 1 M in 388 us against a floor of 162: the sort takes 140,
-// the pieces of the long rows (55 % of the entries) 83, the rows 165, whose chain
+// bf16 rows of 128 into 1 M in 388 to 394 us against a floor of 162: the sort takes
+// 139, the pieces of the long rows (55 % of the entries) 83, the rows 170, whose chain
 // of pointer, entry and row is latency more than bandwidth.
 #include <algorithm>
 
