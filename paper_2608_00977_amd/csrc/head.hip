@@ -39,7 +39,10 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr double kLog2e = 1.4426950408889634074, kLn2 = 0.69314718055994530942;
-constexpr float kOff = -1e9f;    // the exponent of an excluded item
+// The exponent of an excluded item: below that of any other (a bias of -1e7 at
+// temperature 1e-6 is -1.4e13), or blocks of excluded items would be taken for
+// better ones.
+constexpr float kOff = -1e20f;
 // A running maximum before the first item: -5e7 log2 e.  A row whose scores all
 // lie below is empty: its sum stays 0, and none of its items may be had, in the
 // results and in the gradients alike.

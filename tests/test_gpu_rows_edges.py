@@ -237,3 +237,30 @@ def test_an_error_is_reported_once_whichever_stream_met_it(X):
     X.rows_check()
     with torch.cuda.stream(side):
         X.rows_check()
+
+
+@pytest.mark.parametrize("prec", ["fp32", "bf16"])
+@pytest.mark.parametrize("T", [3, 40])
+@pytest.mark.parametrize("n", [3000, 70_000])  # blocks, and groups of blocks
+def test_items_far_below_others_are_better_than_excluded_ones(X, prec, T, n):
+    """Five ordinary items, the first half excluded, the rest biased to -1e9 and less at temperature 0.001."""
+    import torch
+    B, rows = _c(X)
+    k, top = 16, 12
+    H = torch.zeros((T, k), device="cuda").to(torch.float32 if prec == "fp32" else torch.bfloat16)
+    F, _ = _table(np.random.default_rng(n), n, k, prec)
+    b = -1e6 - 16.0 * (np.arange(n) % 1000)  # ties go to the lowest id
+    b[:n // 2] = -np.inf
+    b[n // 2 + 100:n // 2 + 600:100] = [-5.0, -4.0, -3.0, -2.0, -1.0]
+    bias = _gpu(b)
+    want = np.argsort(-b.astype(np.float32), kind="stable")[:top]
+    head = B.tsid_head(rows(H), rows(F), bias.data_ptr(), k, B.BF16 if prec == "bf16" else B.FP32, 1.0, 1e-3)
+    need = B.tsid_score_workspace(T, n, k, head.prec, top)
+    ws, at = _ws(need)
+    ids, logp = torch.empty((T, top), dtype=torch.int32, device="cuda"), torch.empty((T, top), device="cuda")
+    note(f"far below others {prec} T={T} n={n}")
+    assert B.tsid_score(X.ctx, head, None, 0, top, None, None, None, ids.data_ptr(), logp.data_ptr(), at, need,
+                        torch.cuda.current_stream().cuda_stream) == 0
+    assert ids.tolist() == [want.tolist()] * T
+    z = b[want] * 1000.0
+    assert np.allclose(logp.double().cpu().numpy(), z - z[0], rtol=4 * ref.U, atol=1e3 * 8 * ref.U)
