@@ -551,9 +551,10 @@ tsid_status tsid_lookup(tsid_ctx *ctx, int32_t prec, int32_t k, const tsid_rows 
 /* Gradient of tsid_lookup in the table:
  *   dF[i] = scale * sum_(t: ids[t] = i) G[t]    for every row i of dF
  * (rows no id names get zeros).  The ids are sorted on the device (stable; few
- * ids of a short table are looked through instead) and each row of dF is summed in fp32 in an
- * order that the ids alone fix (rows named more than 64 times: in pieces of the
- * sorted list), rounded once and written once.  G->rows < 2^31. */
+ * ids of a short table are looked through instead) and each row of dF is
+ * summed in fp32 in an order that the ids alone fix (rows named more than 64
+ * times: in pieces of the sorted list), rounded once and written once.
+ * G->rows < 2^31. */
 size_t tsid_lookup_grad_workspace(int64_t count, int64_t n, int32_t k);
 tsid_status tsid_lookup_grad(tsid_ctx *ctx, int32_t prec, int32_t k, const tsid_rows *G, const int32_t *ids,
                              float scale, const tsid_rows *dF, void *ws, size_t ws_bytes, void *hip_stream);
